@@ -62,7 +62,7 @@ typedef enum dc_status {
 } dc_status;
 
 enum { DC_PIPE_CONV = 1, DC_PIPE_FLOW = 2, DC_PIPE_VOCODER = 3, DC_PIPE_TOKEN2WAV = 4 };
-enum { DC_F32 = 0, DC_BF16 = 1 };   /* DC_BF16: bf16 storage and operands, fp32 accumulation */
+enum { DC_F32 = 0, DC_BF16 = 1, DC_F16 = 2 };   /* DC_BF16: bf16 storage and operands, fp32 accumulation; DC_F16 (token operators only): the same in fp16 */
 
 /* dc_config.options: switches for tests and measurements.  None of the first four (nor DC_OPT_CTA_PAIRS) changes a result
  * byte; DC_OPT_ROUNDED_NORM selects the other of two admissible roundings.  (There is no configuration
@@ -414,6 +414,89 @@ dc_status dc_test_wavefront_form(const dc_model* model, int* resident_clusters, 
  * (the expected outcome), DC_OK if the wait claimed success, DC_ERR_CUDA on a launch problem.
  * Synchronous; the context stays usable afterwards. */
 dc_status dc_selftest_bounded_wait(int max_polls);
+
+/* ---- The token step in front of the decoder ----------------------------------------------------------------------------
+ *
+ * A speech unit is the autoregressive generation of its tokens followed by the decoder above (paper Section 2.2).  These
+ * operators are the parts of a token model's step that sit between its matrix products: what happens to queries, keys and values
+ * in front of attention, attention itself, and the choice of the next token.  They keep to the conventions at the head of this
+ * file; they allocate nothing per call, need no workspace, and every call can be captured into a CUDA graph and replayed: what
+ * changes from step to step (positions, sequence boundaries, sampling rules, random numbers) is read from device memory.  Calls on different
+ * CUDA streams may overlap as far as the memory that they are given allows.
+ *
+ * A token cache holds keys and values of n_sessions sessions, in memory of the caller:
+ *   k_dev, v_dev : [n_sessions][n_kv_heads][n_sink + ring_rows][head_dim], DC_BF16 or DC_F16
+ * with the retention rule of the flow decoder's carry (Section 3.1, "Two extents"): the row of position p is p for the
+ * first n_sink positions, which are never evicted, and n_sink + (p - n_sink) mod ring_rows behind them.  A token at position q sees
+ * position p if p <= q and (p < n_sink or p > q - window).  A call brings up to ring_rows - window + 1 tokens of a sequence (their
+ * rows must not evict what the first of them sees); longer input is given in pieces.  Rows that no token of a call sees may hold
+ * anything, infinities and NaN included. */
+typedef struct dc_cache dc_cache;
+
+typedef struct dc_cache_config {
+  uint32_t size;                 /* sizeof(dc_cache_config)                                      */
+  int32_t  dtype;                /* DC_BF16 | DC_F16: of the cache and of all rows given with it */
+  int32_t  n_sessions;
+  int32_t  n_heads, n_kv_heads;  /* query heads per key/value head: a whole number, 1 .. 64      */
+  int32_t  head_dim;             /* 64 | 128                                                     */
+  int32_t  n_sink;               /* first tokens that stay visible, >= 0                         */
+  int32_t  window;               /* a token sees itself and the window - 1 tokens before it, >= 1 */
+  int32_t  ring_rows;            /* >= window                                                    */
+} dc_cache_config;
+
+/* The sequences of one call.  Sequence i is session sessions_dev[i] (NULL: i); its tokens are the rows cu_tokens_dev[i] ..
+ * cu_tokens_dev[i + 1] - 1 of the call's matrices, at positions start_dev[i], start_dev[i] + 1, ...  Without
+ * cu_tokens_dev (NULL) sequence i is row i: one token each (n_tokens == n_seqs, max_tokens == 1).  n_tokens is the number of
+ * rows of the matrices, max_tokens the most that one sequence brings.  Rows behind the last sequence are padding: nothing is read or
+ * written there.  The device arrays are read when the work runs; a sequence whose values do not fit (a session
+ * that the cache does not have, a negative position, more tokens than max_tokens or than the ring takes, rows outside of the
+ * matrices) is left out as if it had no tokens.  The sessions of a dc_cache_append call must be distinct. */
+typedef struct dc_token_batch {
+  uint32_t       size;           /* sizeof(dc_token_batch)                                       */
+  int32_t        n_seqs, n_tokens, max_tokens;
+  const int32_t* sessions_dev;   /* [n_seqs] or NULL                                             */
+  const int32_t* cu_tokens_dev;  /* [n_seqs + 1], non-decreasing, or NULL                        */
+  const int32_t* start_dev;      /* [n_seqs]                                                     */
+} dc_token_batch;
+
+/* Norm and rotation of queries and keys: y = x / sqrt(mean(x^2) + eps) * gain for every head, then for j < rot_dim / 2
+ * the pair (y[j], y[j + rot_dim / 2]) - interleaved: (y[2 j], y[2 j + 1]) - turned by the angle position * inv_freq[j]; values
+ * from rot_dim on are not turned.  fp32 inside, the angle in fp64. */
+typedef struct dc_qk_norm {
+  uint32_t     size;             /* sizeof(dc_qk_norm)                                           */
+  int32_t      rot_dim;          /* 0 (no rotation) .. head_dim, a multiple of 16                */
+  int32_t      interleaved;      /* 0 | 1                                                        */
+  float        eps;
+  const float *q_gain_dev, *k_gain_dev;   /* [head_dim], 16-byte aligned                          */
+  const float *inv_freq_dev;              /* [rot_dim / 2]; may be NULL when rot_dim is 0         */
+} dc_qk_norm;
+
+/* Opens a cache over the caller's memory, which stays the caller's and must outlive the handle.  Nothing is written to it: a session
+ * begins with its first token at position 0.  Device: the current one; calls on the cache are made with it current
+ * (DC_ERR_ARG otherwise).  Synchronous; dc_cache_close too. */
+dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void* v_dev, dc_cache** out);
+dc_status dc_cache_close(dc_cache* cache);
+
+/* Waits for the device; DC_ERR_TIMEOUT if a bounded device-side wait of an attention call on this cache has given up since the last check
+ * (the outputs of that call are not valid). */
+dc_status dc_cache_check(dc_cache* cache);
+
+/* Norm and rotation of queries and keys, and the append of keys and values to their sessions' rows, in one pass.
+ *   qkv_dev : [n_tokens] rows of (n_heads + 2 n_kv_heads) * head_dim values - queries, keys, values - qkv_stride values apart
+ *   q_dev   : [n_tokens] rows of n_heads * head_dim values, q_stride values apart; may be qkv_dev itself (same stride):
+ *             the queries are then replaced where they are.  No other overlap.
+ * Strides are multiples of 8 values. */
+dc_status dc_cache_append(dc_cache* cache, const dc_token_batch* batch, const dc_qk_norm* norm, const void* qkv_dev, long long qkv_stride,
+                          void* q_dev, long long q_stride, void* cuda_stream);
+
+/* Attention of the batch's tokens, whose own keys and values have been appended, over their sessions' rows:
+ * out = sum_p w_p v_p / sum_p w_p with w_p = exp(scale * <q, k_p>) over the positions p that the token sees; query head h
+ * reads key/value head h / (n_heads / n_kv_heads).  Scores, sums and outputs are held in fp32 until the one rounding of the result; in
+ * calls of several tokens the numerators are rounded to the cache's type before the product with v.  scale > 0.
+ *   q_dev, out_dev : [n_tokens] rows of n_heads * head_dim values, q_stride / out_stride values apart (multiples of 8).  No overlap with
+ *                    each other or with the cache. */
+dc_status dc_cache_attend(dc_cache* cache, const dc_token_batch* batch, const void* q_dev, long long q_stride, float scale,
+                          void* out_dev, long long out_stride, void* cuda_stream);
 
 const char* dc_status_str(dc_status s);
 

@@ -23,7 +23,8 @@ EXPORTS = ["dc_weights_count", "dc_create", "dc_destroy", "dc_stream_open", "dc_
            "dc_stream_carry_info", "dc_get_counters", "dc_status_str", "dc_last_error",
            "dc_decode_batch_host", "dc_profile_begin", "dc_profile_end", "dc_conv_stack_noalloc",
            "dc_selftest_bounded_wait", "dc_stream_snapshot", "dc_stream_restore", "dc_snapshot_free",
-           "dc_decode_wavefront", "dc_decode_wavefront_batch", "dc_stream_check_guards", "dc_test_fail_allocation", "dc_test_wavefront_form", "dc_measure_fp32_peak"]
+           "dc_decode_wavefront", "dc_decode_wavefront_batch", "dc_stream_check_guards", "dc_test_fail_allocation", "dc_test_wavefront_form", "dc_measure_fp32_peak",
+           "dc_cache_open", "dc_cache_close", "dc_cache_check", "dc_cache_append", "dc_cache_attend"]
 
 
 class dc_config(C.Structure):
@@ -38,6 +39,21 @@ class dc_config(C.Structure):
                 ("f_prompt", C.c_int32), ("f_lookahead", C.c_int32), ("noise_seed_lo", C.c_uint32), ("noise_seed_hi", C.c_uint32),
                 ("cfg_scale", C.c_float), ("max_wave_frames", C.c_int32), ("options", C.c_uint32),
                 ("excitation_std", C.c_float), ("excitation_seed_lo", C.c_uint32), ("excitation_seed_hi", C.c_uint32)]
+
+
+class dc_cache_config(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("dtype", C.c_int32), ("n_sessions", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("n_sink", C.c_int32), ("window", C.c_int32), ("ring_rows", C.c_int32)]
+
+
+class dc_token_batch(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_tokens", C.c_int32),
+                ("sessions_dev", C.c_void_p), ("cu_tokens_dev", C.c_void_p), ("start_dev", C.c_void_p)]
+
+
+class dc_qk_norm(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float),
+                ("q_gain_dev", C.c_void_p), ("k_gain_dev", C.c_void_p), ("inv_freq_dev", C.c_void_p)]
 
 
 class DCError(RuntimeError):
@@ -86,6 +102,11 @@ def load_library():
     lib.dc_measure_fp32_peak.argtypes = [cp(C.c_double)]
     lib.dc_stream_carry_info.argtypes = [vp, cp(C.c_uint64), C.c_int, cp(C.c_int)]
     lib.dc_get_counters.argtypes = [vp, cp(C.c_uint64)]
+    lib.dc_cache_open.argtypes = [cp(dc_cache_config), vp, vp, cp(vp)]
+    lib.dc_cache_close.argtypes = [vp]
+    lib.dc_cache_check.argtypes = [vp]
+    lib.dc_cache_append.argtypes = [vp, vp, vp, vp, C.c_longlong, vp, C.c_longlong, vp]     # (structures by address: the objects below keep them)
+    lib.dc_cache_attend.argtypes = [vp, vp, vp, C.c_longlong, C.c_float, vp, C.c_longlong, vp]
     lib.dc_status_str.restype = C.c_char_p
     lib.dc_status_str.argtypes = [C.c_int]
     lib.dc_last_error.restype = C.c_char_p
@@ -385,3 +406,144 @@ def conv_stack_noalloc(weights_dev, hidden: int, dilations: Sequence[int], x, y,
     d = (C.c_int * len(dilations))(*dilations)
     return lib.dc_conv_stack_noalloc(weights_dev.data_ptr(), hidden, len(dilations), d, x.data_ptr(),
                                      x.shape[0], y.data_ptr(), _cuda_stream_handle(stream))
+
+
+# ---- the token step ------------------------------------------------------------------------------------------------------
+
+
+def _dtype_code(t) -> int:
+    import torch
+    try:
+        return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[t.dtype]
+    except KeyError:
+        raise TypeError(f"{t.dtype} is not served: float32, bfloat16 or float16") from None
+
+
+def _vector(name, t, dtype, n=None, device=None):
+    """Checks a small device array that a call reads; returns its address."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1) or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name}: a contiguous CUDA vector of {dtype}" + (f" and {n} values" if n is not None else "") + f" is wanted, not {tuple(t.shape)} {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    return t.data_ptr()
+
+
+class TokenBatch:
+    """dc_token_batch: the sequences of a call.  start (and sessions, cu_tokens) are CUDA int32 vectors that the program may rewrite in
+    place between calls or graph replays; the object keeps references to them."""
+
+    def __init__(self, sessions, start, cu_tokens=None, n_tokens: Optional[int] = None, max_tokens: int = 1):
+        import torch
+        self.device, n = start.device, start.shape[0]
+        self._kept = (sessions, start, cu_tokens)
+        self.c = c = dc_token_batch()
+        c.size, c.n_seqs, c.max_tokens = C.sizeof(dc_token_batch), n, max_tokens
+        c.n_tokens = n if n_tokens is None else n_tokens
+        c.start_dev = _vector("start", start, torch.int32, n)
+        c.sessions_dev = _vector("sessions", sessions, torch.int32, n, start.device)
+        c.cu_tokens_dev = _vector("cu_tokens", cu_tokens, torch.int32, n + 1, start.device)
+        self.n_tokens, self.address = c.n_tokens, C.addressof(c)
+
+
+class QKNorm:
+    """dc_qk_norm: gains [head_dim] and rotation frequencies [rot_dim / 2], CUDA float32 vectors that the object keeps."""
+
+    def __init__(self, q_gain, k_gain, inv_freq=None, eps: float = 1e-6, interleaved: bool = False):
+        import torch
+        self.device, self.head_dim = q_gain.device, q_gain.shape[0]
+        self._kept = (q_gain, k_gain, inv_freq)
+        self.c = c = dc_qk_norm()
+        c.size, c.eps, c.interleaved = C.sizeof(dc_qk_norm), eps, int(interleaved)
+        c.q_gain_dev = _vector("q_gain", q_gain, torch.float32)
+        c.k_gain_dev = _vector("k_gain", k_gain, torch.float32, self.head_dim, self.device)
+        c.rot_dim = 0 if inv_freq is None else 2 * inv_freq.shape[0]
+        c.inv_freq_dev = _vector("inv_freq", inv_freq, torch.float32, None, self.device)
+        self.address = C.addressof(c)
+
+
+class TokenCache:
+    """dc_cache_open / dc_cache_append / dc_cache_attend: keys and values of many sessions with a sliding window and
+    first tokens that stay, in the caller's tensors k and v [sessions, kv_heads, n_sink + ring_rows, head_dim] (bf16 or fp16)."""
+
+    def __init__(self, k, v, n_heads: int, n_sink: int = 0, window: Optional[int] = None):
+        self.handle = C.c_void_p()
+        for name, t in (("k", k), ("v", v)):
+            if not t.is_cuda or t.dim() != 4 or not t.is_contiguous() or t.shape != k.shape or t.dtype != k.dtype or t.device != k.device:
+                raise ValueError(f"{name}: a contiguous CUDA tensor [sessions, kv_heads, rows, head_dim] is wanted, k and v alike")
+        self.lib, self.k, self.v, self.device, self.dtype = load_library(), k, v, k.device, k.dtype
+        c = dc_cache_config()
+        c.size, c.dtype, c.n_heads, c.n_sink = C.sizeof(dc_cache_config), _dtype_code(k), n_heads, n_sink
+        c.n_sessions, c.n_kv_heads, rows, c.head_dim = k.shape
+        c.ring_rows = rows - n_sink
+        c.window = c.ring_rows if window is None else window
+        self.c_cfg, self.head_dim, self.scale = c, c.head_dim, c.head_dim ** -0.5
+        self._q_width, self._qkv_width = n_heads * c.head_dim, (n_heads + 2 * c.n_kv_heads) * c.head_dim
+        with _on(self.device):
+            _check(self.lib.dc_cache_open(C.byref(c), k.data_ptr(), v.data_ptr(), C.byref(self.handle)), "dc_cache_open")
+        self._h = self.handle.value
+
+    def _rows(self, name, t, width, n):
+        """Checks a matrix of the call ([n, width] or [n, heads, head_dim], rows any stride apart); returns (address, stride)."""
+        if t.dtype != self.dtype or t.device != self.device or t.shape[0] != n or t.numel() != n * width or t.stride(-1) != 1 \
+                or not (t.dim() == 2 or (t.dim() == 3 and t.shape[2] == self.head_dim and t.stride(1) == self.head_dim)):
+            raise ValueError(f"{name}: {n} rows of {width} {self.dtype} values on {self.device} are wanted, not {tuple(t.shape)} {t.dtype} on {t.device}")
+        return t.data_ptr(), t.stride(0) if n > 1 else max(t.stride(0), width)
+
+    def append(self, qkv, batch: TokenBatch, norm: QKNorm, q=None, stream=None):
+        """dc_cache_append: qkv is [n_tokens, (heads + 2 kv_heads) * head_dim]; returns the normalised, rotated queries
+        [n_tokens, heads, head_dim] (in q if given; qkv's own query columns may be given)."""
+        n = batch.n_tokens
+        if q is None:
+            import torch
+            q = torch.empty(n, self.c_cfg.n_heads, self.head_dim, dtype=self.dtype, device=self.device)
+        if batch.device != self.device or norm.device != self.device or norm.head_dim != self.head_dim:
+            raise ValueError("the batch and the norm belong to another device or head_dim than the cache")
+        x, xs = self._rows("qkv", qkv, self._qkv_width, n)
+        y, ys = self._rows("q", q, self._q_width, n)
+        _check(self.lib.dc_cache_append(self._h, batch.address, norm.address, x, xs, y, ys, _token_stream(stream, self.device)), "dc_cache_append")
+        return q
+
+    def attend(self, q, batch: TokenBatch, out=None, scale: Optional[float] = None, stream=None):
+        """dc_cache_attend: q is [n_tokens, heads, head_dim] (or [n_tokens, heads * head_dim]); returns the outputs, in the shape of q."""
+        n = batch.n_tokens
+        if out is None:
+            import torch
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        if batch.device != self.device:
+            raise ValueError("the batch belongs to another device than the cache")
+        x, xs = self._rows("q", q, self._q_width, n)
+        y, ys = self._rows("out", out, self._q_width, n)
+        _check(self.lib.dc_cache_attend(self._h, batch.address, x, xs, self.scale if scale is None else scale, y, ys, _token_stream(stream, self.device)),
+               "dc_cache_attend")
+        return out
+
+    def check(self):
+        """dc_cache_check: waits for the device; raises if a bounded device-side wait of an attention call has given up."""
+        with _on(self.device):
+            _check(self.lib.dc_cache_check(self._h), "dc_cache_check")
+
+    def close(self):
+        if self.handle:
+            _check(self.lib.dc_cache_close(self.handle), "dc_cache_close")
+            self.handle, self._h = C.c_void_p(), None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:      # (the interpreter, or the context, is going)
+            pass
+
+
+def _on(device):
+    import torch
+    return torch.cuda.device(device)
+
+
+def _token_stream(stream, device):
+    """The given stream, or the current one of the tensors' device (which need not be the current device)."""
+    if stream is not None:
+        return stream if isinstance(stream, int) else stream.cuda_stream
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream

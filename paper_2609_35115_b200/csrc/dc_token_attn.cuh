@@ -1,0 +1,396 @@
+// Attention of chunks and prompts over a token cache (dc_cache_attend with several tokens of a sequence): included by
+// dc_token_cache.cu, inside its namespace.
+//
+// Work: 4 D operations per (query head, attended row) against reads of K and V that all queries of a tile share, so a tile of
+// 128 query rows is bound by the tensor cores and by the exponentials, 128 x 64 of each per step.  A tile holds
+// 128 / G tokens with the G query heads that share a key/value head, so short chunks fill it and K/V is read once for the group.
+// Two CTAs per SM, each with 256 columns of tensor memory: scores of two steps (64 columns each; the numerators, rounded to the
+// cache's type, take the place of the scores that they come from and feed the second product from there) and the output.  One warp
+// issues the copies, one the products, four hold a query row per thread: the product of step j + 1 runs under the exponentials of step
+// j.  Keys are taken in the order of the cache's rows, 64 at a time: softmax does not mind their order, so a ring that has wrapped needs no
+// gather, only masks, and steps whose rows no query of the tile sees are left out.
+//
+// The running maximum moves only when a row's new maximum exceeds it by 8 (in powers of two): the numerators then stay below 2^8,
+// within fp16 too, and the output in tensor memory is rescaled in few of the steps.
+
+constexpr int CH_M = 128, CH_N = STEP_N, CH_STAGES = 2, CH_THREADS = 192;
+constexpr uint32_t CH_TMEM = 256, CH_O = 128;   // columns: scores at 0 and 64, output at 128
+
+template <int D>
+constexpr size_t chunk_smem() { return 1024 + (size_t)CH_M * D * 2 + (size_t)CH_STAGES * 2 * CH_N * D * 2; }
+
+struct ChunkArgs {
+  AttendArgs  a;
+  int         tiles;       // of max_tokens
+  CUtensorMap kmap, vmap;  // [sessions * kv_heads * rows][D], boxes of 64 rows x 64 values
+};
+
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t chunk_idesc(int b_mn_major) {
+  // fp32 accumulation, operand types (0: fp16, 1: bf16), N / 8, M / 16
+  return (1u << 4) | (sizeof(T) && Num<T>::is_bf16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(CH_N >> 3) << 17) |
+         ((uint32_t)(CH_M >> 4) << 24);
+}
+// D[tmem] (+)= A[tmem] * B[smem]: a 32-bit column of A holds two neighbouring values of the reduction
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n"
+      "tcgen05.wait::st.sync.aligned;" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+      "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+// The bounded wait (about a second) of a warp: all lanes agree on its outcome, so that what the warp does together stays together.
+constexpr uint32_t CH_POLLS = 1u << 18;
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait_limit(bar, parity, CH_POLLS)); }
+
+struct ChunkBars {
+  uint64_t k_full[CH_STAGES], k_empty[CH_STAGES], v_full[CH_STAGES], v_empty[CH_STAGES];
+  uint64_t s_full[2], p_full[2], q_full;
+  uint64_t pv_done[2];   // of even and odd steps: a row's thread may see step j - 1's product done before it has looked for step j - 2's
+  uint32_t tmem;
+  int      failed;    // a bounded wait gave up
+  int      odd;       // a row of V that some of the tile's queries see and others do not holds an infinity or a NaN
+  float    m[CH_M], l[CH_M];
+};
+
+// One query row with plain arithmetic over the steps' rows: o[0..16) of its columns c0.. .  Only for tiles with odd rows (see ChunkBars),
+// where a weight of zero may not meet a value: here masked rows are not read at all.
+template <typename T, int D>
+__device__ __noinline__ void plain_row(const AttendArgs& a, const T* q, const T* K, const T* V, const RowSet& mine, const StepList& steps, int n, float m, int c0, float* o,
+                                       float* m_out, float* l_out) {
+  float l = 0.f, top = -INFINITY;
+  for (int i = 0; i < 16; ++i) o[i] = 0.f;
+  float base = m == -INFINITY ? 0.f : m;
+  for (int pass = m_out ? 0 : 1; pass < 2; ++pass) {
+    for (int j = 0; j < n; ++j) {
+      const int r0 = steps.tile(j) * CH_N;
+      const uint64_t on = mask64(mine, a.d.n_sink, r0);
+      for (int i = 0; i < CH_N; ++i) {
+        if (!(on >> i & 1)) continue;
+        float s = 0.f;
+        for (int c = 0; c < D; c += 2) {
+          const float2 x = Num<T>::unpack(*reinterpret_cast<const uint32_t*>(q + c)), y = Num<T>::unpack(*reinterpret_cast<const uint32_t*>(K + (long long)(r0 + i) * D + c));
+          s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
+        }
+        s *= a.scale_log2e;
+        if (pass == 0) {
+          top = fmaxf(top, s);
+        } else {
+          const float p = ex2(s - base);
+          l += p;
+          for (int c = 0; c < 16; c += 2) {
+            const float2 v = Num<T>::unpack(*reinterpret_cast<const uint32_t*>(V + (long long)(r0 + i) * D + c0 + c));
+            o[c] = fmaf(p, v.x, o[c]);
+            o[c + 1] = fmaf(p, v.y, o[c + 1]);
+          }
+        }
+      }
+    }
+    if (pass == 0) base = top == -INFINITY ? 0.f : top;
+  }
+  if (m_out) {
+    *m_out = top;
+    *l_out = l;
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __grid_constant__ ChunkArgs args) {
+  constexpr int BOXES = D / 64, QBOX = CH_M * 128, KVBOX = CH_N * 128, KVTILE = BOXES * KVBOX;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ ChunkBars bars;
+  const AttendArgs& a = args.a;
+  uint8_t* smem = smem_raw + ((1024 - (ptx::smem_u32(smem_raw) & 1023)) & 1023);
+  uint8_t *sQ = smem, *sK = sQ + BOXES * QBOX, *sV = sK + CH_STAGES * KVTILE;
+  ptx::pdl_wait();
+  ptx::pdl_launch();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x % a.splits, tile = args.tiles - 1 - blockIdx.x / a.splits;   // late tokens see most rows: first
+  const int kvh = blockIdx.y, G = a.group, per = CH_M / G;
+  const TokenSeq s = load_seq(a.b, a.d, blockIdx.z);
+  const int tok0 = tile * per;
+  if (tok0 >= s.count) return;      // (the whole cluster)
+  const int nt = min(per, s.count - tok0), n_rows = nt * G, q_lo = s.start + tok0, q_hi = q_lo + nt - 1;
+  const int rows = a.d.n_sink + a.d.ring, n_sink = a.d.n_sink;
+  const int plane = (s.session * a.d.n_kv_heads + kvh) * rows;     // (the cache has fewer than 2^31 rows)
+  const RowSet any = seen_by_any(a.d, q_lo, q_hi), all = seen_by_all(a.d, q_lo, q_hi);
+  StepList steps;
+  const int n = steps.build(any, n_sink, rank, a.splits);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < CH_STAGES; ++i) {
+      ptx::mbar_init(&bars.k_full[i], 1);
+      ptx::mbar_init(&bars.k_empty[i], 1);
+      ptx::mbar_init(&bars.v_full[i], 1);
+      ptx::mbar_init(&bars.v_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&bars.s_full[i], 1);
+      ptx::mbar_init(&bars.p_full[i], CH_M);
+      ptx::mbar_init(&bars.pv_done[i], 1);
+    }
+    ptx::mbar_init(&bars.q_full, CH_M);
+    bars.failed = bars.odd = 0;
+    ptx::fence_barrier_init();
+  }
+  if (warp == 5) ptx::tmem_alloc(&bars.tmem, CH_TMEM);
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = bars.tmem;
+
+  const T* Kg = static_cast<const T*>(a.k) + (long long)plane * D;
+  const T* Vg = static_cast<const T*>(a.v) + (long long)plane * D;
+  const T* Qg = static_cast<const T*>(a.q) + (long long)(s.first + tok0) * a.q_stride + (long long)kvh * G * D;
+  bool ok = true;
+  const int tl = threadIdx.x / G, hh = threadIdx.x % G;      // this row's token and head (warps 0 .. 3)
+  const bool live = (int)threadIdx.x < n_rows;
+  RowSet mine = any;
+  float m = -INFINITY, l = 0.f;
+
+  if (warp == 4) {                                           // ---- copies
+    if (ptx::elect_one()) {
+      for (int j = 0; j < n && ok; ++j) {
+        const int st = j % CH_STAGES, y = plane + steps.tile(j) * CH_N;
+        const uint32_t ph = (j / CH_STAGES - 1) & 1;
+        if (j >= CH_STAGES) ok = ptx::mbar_wait_limit(&bars.k_empty[st], ph, CH_POLLS);
+        if (!ok) break;
+        ptx::mbar_expect_tx(&bars.k_full[st], KVTILE);
+#pragma unroll
+        for (int b = 0; b < BOXES; ++b) ptx::tma_load_2d(sK + st * KVTILE + b * KVBOX, &args.kmap, b * 64, y, &bars.k_full[st]);
+        if (j >= CH_STAGES) ok = ptx::mbar_wait_limit(&bars.v_empty[st], ph, CH_POLLS);
+        if (!ok) break;
+        ptx::mbar_expect_tx(&bars.v_full[st], KVTILE);
+#pragma unroll
+        for (int b = 0; b < BOXES; ++b) ptx::tma_load_2d(sV + st * KVTILE + b * KVBOX, &args.vmap, b * 64, y, &bars.v_full[st]);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 5) {                                    // ---- products
+    const uint64_t dq = ptx::umma_desc_sw128(ptx::smem_u32(sQ)), dk = ptx::umma_desc_sw128(ptx::smem_u32(sK)), dv = ptx::umma_desc_sw128(ptx::smem_u32(sV));
+    auto scores = [&](int j) {
+      const int st = j % CH_STAGES;
+      if (!warp_wait(&bars.k_full[st], (j / CH_STAGES) & 1)) return false;
+      ptx::tc_fence_after();
+      if (ptx::elect_one()) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          ptx::umma_bf16(tmem + (j & 1) * CH_N, dq + ((k / 4) * QBOX + (k % 4) * 32) / 16, dk + (st * KVTILE + (k / 4) * KVBOX + (k % 4) * 32) / 16, chunk_idesc<T>(0), k > 0);
+        ptx::umma_commit(&bars.k_empty[st]);
+        ptx::umma_commit(&bars.s_full[j & 1]);
+      }
+      __syncwarp();
+      return true;
+    };
+    ok = warp_wait(&bars.q_full, 0);
+    if (ok && n > 0) ok = scores(0);
+    if (ok && n > 1) ok = scores(1);
+    for (int j = 0; j < n && ok; ++j) {
+      const int st = j % CH_STAGES;
+      ok = warp_wait(&bars.v_full[st], (j / CH_STAGES) & 1) && warp_wait(&bars.p_full[j & 1], (j >> 1) & 1);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      if (ptx::elect_one()) {
+#pragma unroll
+        for (int b = 0; b < BOXES; ++b)
+#pragma unroll
+          for (int k = 0; k < CH_N / 16; ++k)
+            umma_ts(tmem + CH_O + b * 64, tmem + (j & 1) * CH_N + k * 8, dv + (st * KVTILE + b * KVBOX + k * 2048) / 16, chunk_idesc<T>(1), j > 0 || k > 0);
+        ptx::umma_commit(&bars.v_empty[st]);
+        ptx::umma_commit(&bars.pv_done[j & 1]);
+      }
+      __syncwarp();
+      if (j + 2 < n) ok = scores(j + 2);      // (into the columns that the product above has just read: products run in order)
+    }
+  } else {                                                   // ---- a query row per thread
+    // the queries, 16 bytes a lane, to the swizzled rows that the products read
+    constexpr int CPR = D / 8;
+#pragma unroll
+    for (int i = 0; i < CPR; ++i) {
+      const int ch = i * 32 + lane, r = warp * 32 + ch / CPR, c = ch % CPR;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (r < n_rows) v = *reinterpret_cast<const uint4*>(Qg + (long long)(r / G) * a.q_stride + (r % G) * D + c * 8);
+      *reinterpret_cast<uint4*>(sQ + (c / 8) * QBOX + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+    }
+    ptx::fence_proxy_async_smem();
+    ptx::mbar_arrive(&bars.q_full);
+    const int qp = q_lo + (live ? tl : 0);
+    mine = seen_by_any(a.d, qp, qp);
+    const uint32_t lane_base = tmem + ((uint32_t)warp << 21);      // lanes 32 warp .. of tensor memory
+    for (int j = 0; j < n; ++j) {
+      const int r0 = steps.tile(j) * CH_N, st = j % CH_STAGES;
+      ok = warp_wait(&bars.s_full[j & 1], (j >> 1) & 1) && (j < 2 || warp_wait(&bars.pv_done[j & 1], ((j - 2) >> 1) & 1));    // (the second: step j - 2's, long done: no phase goes by unseen)
+      if (!ok) break;
+      ptx::tc_fence_after();
+      float x[CH_N];
+      ptx::tmem_ld64(lane_base + (j & 1) * CH_N, x);
+      const uint64_t in_all = mask64(all, n_sink, r0);
+      if (in_all != ~0ull) {                                 // some query of the tile does not see some row
+        const uint64_t on = mask64(mine, n_sink, r0), in_any = mask64(any, n_sink, r0);
+#pragma unroll
+        for (int i = 0; i < CH_N; ++i) x[i] = (i < 32 ? (uint32_t)on >> i : (uint32_t)(on >> 32) >> (i - 32)) & 1 ? x[i] : -INFINITY;
+        // rows of V that nobody sees become zeros; of those that only some see, infinities and NaN are noted
+        ok = warp_wait(&bars.v_full[st], (j / CH_STAGES) & 1);
+        if (!ok) break;
+        bool odd = false;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < CH_N * CPR; i += CH_M) {
+          const int r = i / CPR, c = i % CPR;
+          if (in_all >> r & 1) continue;
+          uint4* p = reinterpret_cast<uint4*>(sV + st * KVTILE + (c / 8) * KVBOX + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+          if (in_any >> r & 1) {
+            const uint4 v = *p;
+            odd |= Num<T>::odd(v.x) | Num<T>::odd(v.y) | Num<T>::odd(v.z) | Num<T>::odd(v.w);
+          } else {
+            *p = make_uint4(0, 0, 0, 0);
+          }
+        }
+        if (odd) bars.odd = 1;
+        ptx::fence_proxy_async_smem();
+      }
+      float t0 = x[0], t1 = x[1], t2 = x[2], t3 = x[3];
+#pragma unroll
+      for (int i = 4; i < CH_N; i += 4) {
+        t0 = fmaxf(t0, x[i]);
+        t1 = fmaxf(t1, x[i + 1]);
+        t2 = fmaxf(t2, x[i + 2]);
+        t3 = fmaxf(t3, x[i + 3]);
+      }
+      const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * a.scale_log2e;
+      const bool move = top > m + 8.f;                       // (m = -inf: at the first row that is seen)
+      if (__any_sync(0xffffffffu, move)) {
+        const float f = move ? ex2(m - top) : 1.f;
+        if (move) m = top;
+        l *= f;
+        if (j > 0) {
+          ok = warp_wait(&bars.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1);
+          if (!ok) break;
+          ptx::tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            float o[16];
+            ptx::tmem_ld16(lane_base + CH_O + c, o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] *= f;
+            ptx::tmem_st16(lane_base + CH_O + c, o);
+          }
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      const float2 sc2 = make_float2(a.scale_log2e, a.scale_log2e), nb2 = make_float2(-base, -base);
+      float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+      uint32_t p[CH_N / 2];
+#pragma unroll
+      for (int i = 0; i < CH_N; i += 4) {
+        float2 u = fma2(make_float2(x[i], x[i + 1]), sc2, nb2), v = fma2(make_float2(x[i + 2], x[i + 3]), sc2, nb2);
+        u = make_float2(ex2(u.x), ex2(u.y));
+        v = make_float2(ex2(v.x), ex2(v.y));
+        sum0 = add2(sum0, u);
+        sum1 = add2(sum1, v);
+        p[i / 2] = Num<T>::pack(u.x, u.y);
+        p[i / 2 + 1] = Num<T>::pack(v.x, v.y);
+      }
+      sum0 = add2(sum0, sum1);
+      l += sum0.x + sum0.y;
+      tmem_st32(lane_base + (j & 1) * CH_N, p);
+      ptx::tc_fence_before();
+      ptx::mbar_arrive(&bars.p_full[j & 1]);
+    }
+    if (ok && n > 1) ok = warp_wait(&bars.pv_done[n & 1], ((n - 2) >> 1) & 1);
+    if (ok && n > 0) ok = warp_wait(&bars.pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
+    ptx::tc_fence_after();
+  }
+  if (!ok) {
+    bars.failed = 1;
+    *a.err = 1;
+  }
+  __syncthreads();                                           // every product of this CTA has completed, or a wait has given up
+  if (bars.failed) {
+    ptx::pause_for_copies();
+  } else if (warp < 4) {
+    const bool odd = bars.odd != 0;
+    const uint32_t lane_base = tmem + ((uint32_t)warp << 21);
+    const T* q = Qg + (long long)(live ? tl : 0) * a.q_stride + (live ? hh : 0) * D;
+    T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + (live ? tl : 0)) * a.out_stride + (long long)(kvh * G + (live ? hh : 0)) * D;
+    float* part = reinterpret_cast<float*>(sK);              // [128][D], 16-byte pieces of a row in the order piece ^ (row & 15)
+#pragma unroll 1
+    for (int c = 0; c < D; c += 16) {
+      float o[16];
+      if (n == 0) {
+        for (int i = 0; i < 16; ++i) o[i] = 0.f;
+      } else if (odd) {
+        plain_row<T, D>(a, q, Kg, Vg, mine, steps, n, m, c, o, c == 0 ? &m : nullptr, &l);
+      } else {
+        ptx::tmem_ld16(lane_base + CH_O + c, o);
+      }
+      if (a.splits == 1) {
+        const float inv = 1.0f / l;
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = Num<T>::pack(o[2 * i] * inv, o[2 * i + 1] * inv);
+        if (live) {
+          *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(part + threadIdx.x * D + (((c / 4 + i) ^ (threadIdx.x & 15)) << 2)) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+      }
+    }
+    bars.m[threadIdx.x] = m;
+    bars.l[threadIdx.x] = l;
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 5) ptx::tmem_dealloc(tmem, CH_TMEM);
+  if (a.splits == 1) return;
+  ptx::cluster_arrive();
+  ptx::cluster_wait();
+  // join: the cluster's CTAs share the tile's elements out, four columns a thread
+  const uint32_t part_s = ptx::smem_u32(sK), m_s = ptx::smem_u32(bars.m), l_s = ptx::smem_u32(bars.l);
+  for (int e = rank * CH_THREADS + threadIdx.x; e < n_rows * (D / 4); e += a.splits * CH_THREADS) {
+    const int r = e / (D / 4), c = e % (D / 4);
+    float M = -INFINITY;
+    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, ld_cluster(ptx::map_to_cta(m_s + r * 4, k)));
+    const float base = M == -INFINITY ? 0.f : M;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float L = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < a.splits; ++k) {
+      const float f = ex2(ld_cluster(ptx::map_to_cta(m_s + r * 4, k)) - base);
+      const float4 v = ld_cluster4(ptx::map_to_cta(part_s + (r * D + ((c ^ (r & 15)) << 2)) * 4, k));
+      o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));
+      L = fmaf(f, ld_cluster(ptx::map_to_cta(l_s + r * 4, k)), L);
+    }
+    const float inv = 1.0f / L;
+    T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + r / G) * a.out_stride + (long long)(kvh * G + r % G) * D + c * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(Num<T>::pack(o.x * inv, o.y * inv), Num<T>::pack(o.z * inv, o.w * inv));
+  }
+  ptx::cluster_arrive();      // no CTA's shared memory goes while another reads it
+  ptx::cluster_wait();
+}

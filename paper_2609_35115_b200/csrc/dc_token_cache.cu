@@ -1,0 +1,707 @@
+// The operators over a token cache (include/dc.h): norms and rotation of queries and keys with the append of keys and values,
+// and attention with a sliding window and first tokens that stay visible.  This file holds the boundary, the append and the
+// attention of single tokens; dc_token_attn.cuh the attention of chunks.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include <new>
+
+#include "dc_internal.h"
+#include "dc_ptx.cuh"
+#include "dc_token_cache.h"
+
+namespace dc {
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+template <typename T> struct Num;
+template <> struct Num<bf16> {
+  static constexpr bool is_bf16 = true;
+  // whether one of the two values is an infinity or a NaN
+  static __device__ __forceinline__ bool odd(uint32_t v) { return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u; }
+  static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+};
+template <> struct Num<__half> {
+  static constexpr bool is_bf16 = false;
+  static __device__ __forceinline__ bool odd(uint32_t v) { return (v & 0x7c00u) == 0x7c00u || (v & 0x7c000000u) == 0x7c000000u; }
+  static __device__ __forceinline__ float2 unpack(uint32_t v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  }
+};
+
+__device__ __forceinline__ void unpack8(const uint4& v, float* x, bf16) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = Num<bf16>::unpack(w[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void unpack8(const uint4& v, float* x, __half) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = Num<__half>::unpack(w[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Append: y = x / sqrt(mean x^2 + eps) * g for each head of q and k, rotated by position * inv_freq; k and v to their rows.
+// ---------------------------------------------------------------------------------------------
+struct AppendArgs {
+  CacheDims   d;
+  TokenBatch  b;
+  const void* qkv;
+  long long   qkv_stride, q_stride;
+  void *      q, *k, *v;
+  const float *q_gain, *k_gain, *inv_freq;
+  int         rot;
+  float       eps;
+};
+
+constexpr int APPEND_THREADS = 256;
+constexpr int APPEND_MAX_CHUNKS = 4;   // 16-byte pieces of a row that a thread has in flight
+
+// One CTA per token.  A head is D / 8 neighbouring lanes of 16 bytes each, so the sum of squares and the partner of a
+// rotated pair come from shuffles and every value is read once and written once.  The angle is position * inv_freq in
+// 64 bits, in turns, whose fraction is exact enough in 32 for sincospi: rot / 2 of them per token, shared by all heads.
+template <typename T, int D, bool INTER>
+__global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs a) {
+  constexpr int LPH = D / 8;
+  __shared__ float2 turn[D / 2];
+  ptx::pdl_wait();
+  ptx::pdl_launch();
+  const int token = blockIdx.x, lane = threadIdx.x & 31, half = a.rot / 2;
+  // the token's sequence: the boundaries at or below it, counted 32 at a time
+  int seq = token;
+  if (a.b.cu_tokens) {
+    seq = -1;
+    for (int i0 = 0; i0 <= a.b.n_seqs; i0 += 32) {
+      const int c = i0 + lane <= a.b.n_seqs ? a.b.cu_tokens[i0 + lane] : INT_MAX;
+      const unsigned le = __ballot_sync(0xffffffffu, c <= token);
+      seq += __popc(le);
+      if (le != 0xffffffffu) break;
+    }
+    if (seq < 0 || seq >= a.b.n_seqs) return;   // a row behind the last sequence
+  }
+  const TokenSeq s = load_seq(a.b, a.d, seq);
+  if (token - s.first >= s.count || token < s.first) return;
+  const int pos = s.start + (token - s.first);
+  if ((int)threadIdx.x < half) {
+    const double t = (double)pos * (double)a.inv_freq[threadIdx.x] * 0.15915494309189533577;
+    float sn, cs;
+    sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
+    turn[threadIdx.x] = make_float2(cs, sn);
+  }
+  const int H = a.d.n_heads, Hkv = a.d.n_kv_heads, chunks = (H + 2 * Hkv) * LPH;
+  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.qkv) + (long long)token * a.qkv_stride);
+  const long long row = cache_row(a.d, pos), rows = a.d.n_sink + a.d.ring;
+  const int l = threadIdx.x % LPH;
+  bool synced = false;
+  for (int c0 = 0; c0 < chunks; c0 += APPEND_MAX_CHUNKS * blockDim.x) {
+    uint4 in[APPEND_MAX_CHUNKS];
+#pragma unroll
+    for (int u = 0; u < APPEND_MAX_CHUNKS; ++u) {
+      const int c = c0 + u * (int)blockDim.x + (int)threadIdx.x;
+      in[u] = c < chunks ? src[c] : make_uint4(0, 0, 0, 0);
+    }
+    if (!synced) __syncthreads();
+    synced = true;
+#pragma unroll
+    for (int u = 0; u < APPEND_MAX_CHUNKS; ++u) {
+      const int c = c0 + u * (int)blockDim.x + (int)threadIdx.x, head = c / LPH;
+      if (c - lane >= chunks) break;   // (the whole warp)
+      uint4 out = in[u];
+      // a warp's pieces may belong to q or k and to v at once (head_dim 64: four heads of a warp): all lanes go through the shuffles
+      float x[8], ss = 0.f;
+      unpack8(in[u], x, T());
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+#pragma unroll
+      for (int m = LPH / 2; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+      const float r = rsqrtf(ss * (1.0f / D) + a.eps);
+      const float4* g = reinterpret_cast<const float4*>(head < H ? a.q_gain : a.k_gain) + 2 * l;
+      const float4 g0 = __ldg(g), g1 = __ldg(g + 1);
+      const float gain[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = x[i] * r * gain[i];
+      if (INTER) {
+        if (8 * l < a.rot) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 t = turn[4 * l + i];
+            const float p = x[2 * i], q = x[2 * i + 1];
+            x[2 * i] = p * t.x - q * t.y;
+            x[2 * i + 1] = q * t.x + p * t.y;
+          }
+        }
+      } else {
+        const int hl = half / 8;   // lanes of half a rotated head
+        const bool lower = l < hl;
+        const int partner = lane + (lower ? hl : l < 2 * hl ? -hl : 0);
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = __shfl_sync(0xffffffffu, x[i], partner);
+        if (l < 2 * hl) {
+          const float2* t = turn + 8 * (lower ? l : l - hl);
+          const float sign = lower ? -1.f : 1.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = x[i] * t[i].x + sign * (o[i] * t[i].y);
+        }
+      }
+      if (head < H + Hkv)
+        out = make_uint4(Num<T>::pack(x[0], x[1]), Num<T>::pack(x[2], x[3]), Num<T>::pack(x[4], x[5]), Num<T>::pack(x[6], x[7]));
+      if (c >= chunks) continue;
+      T* dst;
+      if (head < H) {
+        dst = static_cast<T*>(a.q) + (long long)token * a.q_stride + (long long)head * D;
+      } else {
+        const int h = head < H + Hkv ? head - H : head - H - Hkv;
+        dst = static_cast<T*>(head < H + Hkv ? a.k : a.v) + (((long long)s.session * Hkv + h) * rows + row) * D;
+      }
+      reinterpret_cast<uint4*>(dst)[l] = out;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention of single tokens: one query row per head against the rows of its window and the first tokens.
+// ---------------------------------------------------------------------------------------------
+struct AttendArgs {
+  CacheDims   d;
+  TokenBatch  b;
+  const void *q, *k, *v;
+  void*       out;
+  long long   q_stride, out_stride;
+  float       scale_log2e;
+  int         group;     // query heads of a key/value head
+  int         splits;    // CTAs of a cluster
+  int*        err;
+};
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16816<bf16>(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16816<__half>(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+constexpr int STEP_WARPS = 4;
+constexpr int STEP_STAGES = 3;
+constexpr int STEP_HALF = 4096;                         // bytes of K, and of V, in a unit
+constexpr int STEP_UNIT = 2 * STEP_HALF;
+constexpr int STEP_SMEM = STEP_WARPS * STEP_STAGES * STEP_UNIT;
+constexpr int STEP_ROWS = 16;                           // query heads that one CTA serves (the rows of its products)
+
+// Bound by the reads of K and V, so the work is laid out for loads: a unit is 4 KB of K rows and the same V rows (16 rows of 128
+// values, 32 of 64), every warp streams units of its own through three stages of asynchronous 16-byte copies and keeps its own
+// running maximum, sum and output in registers; no warp waits for another before the end.  The query heads that share a K/V head are
+// the 16 rows of the matrix products (m16n8k16), so a row of K and V is read once for all of them.  The units of a
+// (sequence, head) are dealt out over the warps of a cluster of CTAs, which joins the partial results through distributed shared
+// memory: no workspace, no second launch.  The numerators enter the second product as two halves (their rounding to 16 bits and what
+// that leaves): the products are a tenth of the time that the reads take.
+template <typename T, int D>
+__global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const AttendArgs a) {
+  constexpr int UN = STEP_HALF / (2 * D);    // rows of a unit
+  constexpr int CPR = D / 8;                 // 16-byte chunks of a row
+  constexpr int NT = UN / 8, KS = D / 16, DT = D / 8;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ float wm[STEP_WARPS][STEP_ROWS], wl[STEP_WARPS][STEP_ROWS];
+  __shared__ float cm[STEP_ROWS], cl[STEP_ROWS];
+  ptx::pdl_wait();
+  ptx::pdl_launch();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int rank = blockIdx.x;   // in the cluster: gridDim.x == splits
+  const int groups = (a.group + STEP_ROWS - 1) / STEP_ROWS;
+  const int kvh = blockIdx.y / groups, h0 = (blockIdx.y % groups) * STEP_ROWS, nh = min(STEP_ROWS, a.group - h0);
+  const TokenSeq s = load_seq(a.b, a.d, blockIdx.z);
+  if (s.count != 1) return;      // (the whole cluster)
+  const int pos = s.start, rows = a.d.n_sink + a.d.ring;
+  const RowRuns run = row_runs(a.d, pos);
+  const int n_first = run.n_first, lo2 = run.lo_second, n_second = run.n_second;
+  const int u_first = (n_first + UN - 1) / UN, units = u_first + (n_second + UN - 1) / UN;
+  const long long plane = ((long long)s.session * a.d.n_kv_heads + kvh) * rows;
+  const T* K = static_cast<const T*>(a.k) + plane * D;
+  const T* V = static_cast<const T*>(a.v) + plane * D;
+
+  uint8_t* ring = smem + warp * STEP_STAGES * STEP_UNIT;
+  const uint32_t ring_s = ptx::smem_u32(ring);
+  const int step = a.splits * STEP_WARPS;
+  auto unit_rows = [&](int u, int& row0) {
+    row0 = u < u_first ? u * UN : lo2 + (u - u_first) * UN;
+    return u < u_first ? n_first - row0 : n_second - (u - u_first) * UN;   // (may exceed UN)
+  };
+  auto fetch = [&](int u, int stage) {
+    if (u < units) {
+      int row0;
+      const int n = unit_rows(u, row0);
+      const uint32_t dst = ring_s + stage * STEP_UNIT;
+#pragma unroll
+      for (int i = 0; i < UN * CPR / 32; ++i) {
+        const int ch = i * 32 + lane, r = ch / CPR, c = ch % CPR;
+        const bool on = r < n;     // rows behind the run read as zeros: whatever they hold must not meet a weight of zero
+        const long long off = on ? (long long)(row0 + r) * D + c * 8 : 0;
+        const uint32_t at = dst + r * (2 * D) + ((c ^ (r & 7)) << 4);
+        cp16(at, K + off, on);
+        cp16(at + STEP_HALF, V + off, on);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int u = rank * STEP_WARPS + warp;
+#pragma unroll
+  for (int i = 0; i < STEP_STAGES - 1; ++i) fetch(u + i * step, i);
+
+  // the queries as the first operand: rows g and g + 8
+  uint32_t qf[KS][4];
+  {
+    const T* q = static_cast<const T*>(a.q) + (long long)s.first * a.q_stride + (long long)(kvh * a.group + h0) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = g + (i & 1) * 8, c = ks * 16 + t * 2 + (i >> 1) * 8;
+        qf[ks][i] = r < nh ? *reinterpret_cast<const uint32_t*>(q + r * D + c) : 0u;
+      }
+  }
+  float o[DT][4];
+#pragma unroll
+  for (int j = 0; j < DT; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+  int stage = 0;
+  for (; u < units; u += step) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(STEP_STAGES - 2) : "memory");
+    __syncwarp();    // the other lanes' copies of this unit have landed, and all have read the stage that is filled next
+    fetch(u + (STEP_STAGES - 1) * step, stage == 0 ? STEP_STAGES - 1 : stage - 1);
+    const uint32_t ks_ = ring_s + stage * STEP_UNIT, vs_ = ks_ + STEP_HALF;
+    stage = stage + 1 == STEP_STAGES ? 0 : stage + 1;
+    int row0;
+    const int n = unit_rows(u, row0);
+    float sc[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[j][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int j = 0; j < NT; j += 2) {
+        uint32_t kf[4];
+        const int r = (j + (lane >> 4)) * 8 + (lane & 7), c = 2 * ks + ((lane >> 3) & 1);
+        ldsm4(ks_ + r * (2 * D) + ((c ^ (r & 7)) << 4), kf);
+        mma16816<T>(sc[j], qf[ks], kf[0], kf[1]);
+        mma16816<T>(sc[j + 1], qf[ks], kf[2], kf[3]);
+      }
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = j * 8 + t * 2 + (i & 1) < n ? sc[j][i] * a.scale_log2e : -INFINITY;
+        sc[j][i] = x;
+        top[i >> 1] = fmaxf(top[i >> 1], x);
+      }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+    }
+    if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float mn = fmaxf(m[i], top[i]);
+        const float f = mn > m[i] ? ex2(m[i] - mn) : 1.f;     // (m = -inf: 0)
+        m[i] = mn;
+        l[i] *= f;
+#pragma unroll
+        for (int j = 0; j < DT; ++j) {
+          o[j][2 * i] *= f;
+          o[j][2 * i + 1] *= f;
+        }
+      }
+    }
+    const float base[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[j][i] = ex2(sc[j][i] - base[i >> 1]);
+        l[i >> 1] += sc[j][i];
+      }
+#pragma unroll
+    for (int kk = 0; kk < NT / 2; ++kk) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = sc[2 * kk + (i >> 1)][(i & 1) * 2], y = sc[2 * kk + (i >> 1)][(i & 1) * 2 + 1];
+        hi[i] = Num<T>::pack(x, y);
+        const float2 r = Num<T>::unpack(hi[i]);
+        lo[i] = Num<T>::pack(x - r.x, y - r.y);
+      }
+#pragma unroll
+      for (int j = 0; j < DT; j += 2) {
+        uint32_t vf[4];
+        const int r = kk * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), c = j + (lane >> 4);
+        ldsm4t(vs_ + r * (2 * D) + ((c ^ (r & 7)) << 4), vf);
+        mma16816<T>(o[j], hi, vf[0], vf[1]);
+        mma16816<T>(o[j + 1], hi, vf[2], vf[3]);
+        mma16816<T>(o[j], lo, vf[0], vf[1]);
+        mma16816<T>(o[j + 1], lo, vf[2], vf[3]);
+      }
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncwarp();
+
+  // ---- join: the warps of the CTA, then the CTAs of the cluster -----------------------------------------------------------
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+    if (t == 0) {
+      wm[warp][g + 8 * i] = m[i];
+      wl[warp][g + 8 * i] = l[i];
+    }
+  }
+  float* part = reinterpret_cast<float*>(ring);     // [16][D] of this warp (8 KB of its 24)
+#pragma unroll
+  for (int j = 0; j < DT; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (g + 8 * i < nh) *reinterpret_cast<float2*>(part + (g + 8 * i) * D + j * 8 + t * 2) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+  __syncthreads();
+  constexpr int WSTRIDE = STEP_STAGES * STEP_UNIT / 4;   // floats between two warps' parts
+  float* all = reinterpret_cast<float*>(smem);
+  T* out = static_cast<T*>(a.out) + (long long)s.first * a.out_stride + (long long)(kvh * a.group + h0) * D;
+  for (int e = threadIdx.x * 2; e < nh * D; e += STEP_WARPS * 64) {
+    const int r = e / D;
+    float M = wm[0][r];
+#pragma unroll
+    for (int w = 1; w < STEP_WARPS; ++w) M = fmaxf(M, wm[w][r]);
+    const float base = M == -INFINITY ? 0.f : M;
+    float x = 0.f, y = 0.f, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < STEP_WARPS; ++w) {
+      const float f = ex2(wm[w][r] - base);
+      const float2 v = *reinterpret_cast<const float2*>(all + w * WSTRIDE + e);
+      x = fmaf(f, v.x, x);
+      y = fmaf(f, v.y, y);
+      L = fmaf(f, wl[w][r], L);
+    }
+    if (a.splits == 1) {
+      const float inv = 1.0f / L;
+      *reinterpret_cast<uint32_t*>(out + e) = Num<T>::pack(x * inv, y * inv);
+    } else {
+      *reinterpret_cast<float2*>(all + e) = make_float2(x, y);     // (each element is read and written by one thread)
+      if (e % D == 0) {
+        cm[r] = M;
+        cl[r] = L;
+      }
+    }
+  }
+  if (a.splits == 1) return;
+  ptx::cluster_arrive();
+  ptx::cluster_wait();
+  const uint32_t all_s = ptx::smem_u32(all), cm_s = ptx::smem_u32(cm), cl_s = ptx::smem_u32(cl);
+  for (int e = (rank * STEP_WARPS * 32 + (int)threadIdx.x) * 2; e < nh * D; e += a.splits * STEP_WARPS * 64) {
+    const int r = e / D;
+    float M = -INFINITY;
+    for (int c = 0; c < a.splits; ++c) M = fmaxf(M, ld_cluster(ptx::map_to_cta(cm_s + r * 4, c)));
+    const float base = M == -INFINITY ? 0.f : M;
+    float x = 0.f, y = 0.f, L = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < a.splits; ++c) {
+      const float f = ex2(ld_cluster(ptx::map_to_cta(cm_s + r * 4, c)) - base);
+      const uint32_t at = ptx::map_to_cta(all_s + e * 4, c);
+      x = fmaf(f, ld_cluster(at), x);
+      y = fmaf(f, ld_cluster(at + 4), y);
+      L = fmaf(f, ld_cluster(ptx::map_to_cta(cl_s + r * 4, c)), L);
+    }
+    const float inv = 1.0f / L;
+    *reinterpret_cast<uint32_t*>(out + e) = Num<T>::pack(x * inv, y * inv);
+  }
+  ptx::cluster_arrive();      // no CTA's shared memory goes while another reads it
+  ptx::cluster_wait();
+}
+
+#include "dc_token_attn.cuh"
+
+template <typename K>
+cudaError_t launch(K kernel, dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const void* arg) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = 1;
+  if (cluster > 1) {
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+  }
+  cfg.attrs = attr;
+  void* args[] = {const_cast<void*>(arg)};
+  return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), args);
+}
+
+bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+}  // namespace
+}  // namespace dc
+
+struct dc_cache {
+  dc::CacheDims d;
+  int   head_dim, dtype, device, n_sm;
+  void *k, *v;
+  int*  err;      // device word that a bounded wait sets when it gives up
+  CUtensorMap kmap, vmap;
+};
+
+#define DC_REFUSE(code, ...)    \
+  do {                          \
+    dc::set_error(__VA_ARGS__); \
+    return code;                \
+  } while (0)
+
+namespace {
+
+// Everything that can be told about a batch without the device's values.
+dc_status admit_batch(const dc_cache* c, const dc_token_batch* b, const char* who) {
+  if (!c || !b) DC_REFUSE(DC_ERR_ARG, "%s: null pointer argument", who);
+  if (b->size != sizeof(dc_token_batch)) DC_REFUSE(DC_ERR_ARG, "%s: dc_token_batch.size is %u, this library's is %zu", who, b->size, sizeof(dc_token_batch));
+  if (b->n_seqs < 1 || b->n_seqs > 65535 || b->n_tokens < 1 || b->max_tokens < 1)
+    DC_REFUSE(DC_ERR_ARG, "%s: need 1 <= n_seqs <= 65535, n_tokens >= 1, max_tokens >= 1", who);
+  if (!b->start_dev) DC_REFUSE(DC_ERR_ARG, "%s: start_dev is null", who);
+  if (!b->cu_tokens_dev && (b->max_tokens != 1 || b->n_tokens != b->n_seqs))
+    DC_REFUSE(DC_ERR_ARG, "%s: without cu_tokens_dev every sequence brings one token (n_tokens == n_seqs, max_tokens == 1)", who);
+  if (!b->sessions_dev && b->n_seqs > c->d.n_sessions)
+    DC_REFUSE(DC_ERR_ARG, "%s: %d sequences without sessions_dev, the cache has %d sessions", who, b->n_seqs, c->d.n_sessions);
+  if ((long long)b->max_tokens > (long long)c->d.ring - c->d.window + 1)
+    DC_REFUSE(DC_ERR_FRAMES, "%s: %d tokens of a sequence in one call, a ring of %d rows with a window of %d takes %d", who, b->max_tokens, c->d.ring,
+              c->d.window, c->d.ring - c->d.window + 1);
+  int dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) DC_REFUSE(DC_ERR_CUDA, "%s: cudaGetDevice failed: %s", who, cudaGetErrorString(e));
+  if (dev != c->device) DC_REFUSE(DC_ERR_ARG, "%s: the cache is on device %d, the current device is %d", who, c->device, dev);
+  return DC_OK;
+}
+
+bool bad_rows(const void* p, long long stride, long long width) { return !p || dc::misaligned(p) || stride < width || stride % 8; }
+
+dc_status launched(cudaError_t e, const char* who) {
+  if (e != cudaSuccess) {
+    cudaGetLastError();   // (a refused launch leaves its code behind)
+    DC_REFUSE(DC_ERR_CUDA, "%s: launch failed: %s", who, cudaGetErrorString(e));
+  }
+  return DC_OK;
+}
+
+dc::TokenBatch kernel_batch(const dc_token_batch* b) {
+  return dc::TokenBatch{b->n_seqs, b->n_tokens, b->max_tokens, b->sessions_dev, b->cu_tokens_dev, b->start_dev};
+}
+
+using AppendFn = void (*)(const dc::AppendArgs);
+using StepFn = void (*)(const dc::AttendArgs);
+AppendFn append_fn(int dtype, int D, bool inter) {
+  using namespace dc;
+  if (dtype == DC_BF16) return D == 128 ? (inter ? append_kernel<bf16, 128, true> : append_kernel<bf16, 128, false>)
+                                        : (inter ? append_kernel<bf16, 64, true> : append_kernel<bf16, 64, false>);
+  return D == 128 ? (inter ? append_kernel<__half, 128, true> : append_kernel<__half, 128, false>)
+                  : (inter ? append_kernel<__half, 64, true> : append_kernel<__half, 64, false>);
+}
+StepFn step_fn(int dtype, int D) {
+  using namespace dc;
+  if (dtype == DC_BF16) return D == 128 ? attend_step_kernel<bf16, 128> : attend_step_kernel<bf16, 64>;
+  return D == 128 ? attend_step_kernel<__half, 128> : attend_step_kernel<__half, 64>;
+}
+
+using ChunkFn = void (*)(const dc::ChunkArgs);
+ChunkFn chunk_fn(int dtype, int D) {
+  using namespace dc;
+  if (dtype == DC_BF16) return D == 128 ? attend_chunk_kernel<bf16, 128> : attend_chunk_kernel<bf16, 64>;
+  return D == 128 ? attend_chunk_kernel<__half, 128> : attend_chunk_kernel<__half, 64>;
+}
+size_t chunk_smem_bytes(int D) { return D == 128 ? dc::chunk_smem<128>() : dc::chunk_smem<64>(); }
+
+// The cache as one matrix of rows, fetched in boxes of 64 rows and 64 values in the 128-byte swizzle.
+bool cache_map(CUtensorMap* m, const dc_cache* c, void* base) {
+  using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) return false;
+  const cuuint64_t dim[2] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->d.n_sessions * c->d.n_kv_heads * (c->d.n_sink + c->d.ring)}, stride[1] = {(cuuint64_t)c->head_dim * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)dc::CH_N}, one[2] = {1, 1};
+  return reinterpret_cast<EncodeFn>(fn)(m, c->dtype == DC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dim, stride, box, one,
+                                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void* v_dev, dc_cache** out) {
+  if (!out) DC_REFUSE(DC_ERR_ARG, "dc_cache_open: null pointer argument");
+  *out = nullptr;
+  if (!cfg || !k_dev || !v_dev) DC_REFUSE(DC_ERR_ARG, "dc_cache_open: null pointer argument");
+  if (cfg->size != sizeof(dc_cache_config)) DC_REFUSE(DC_ERR_CONFIG, "dc_cache_open: dc_cache_config.size is %u, this library's is %zu", cfg->size, sizeof(dc_cache_config));
+  if (cfg->dtype != DC_BF16 && cfg->dtype != DC_F16) DC_REFUSE(DC_ERR_CONFIG, "dc_cache_open: a cache holds DC_BF16 or DC_F16");
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) DC_REFUSE(DC_ERR_CONFIG, "dc_cache_open: head_dim is %d, 64 and 128 are served", cfg->head_dim);
+  if (cfg->n_kv_heads < 1 || cfg->n_heads < cfg->n_kv_heads || cfg->n_heads % cfg->n_kv_heads || cfg->n_heads / cfg->n_kv_heads > 64 || cfg->n_heads > 1024)
+    DC_REFUSE(DC_ERR_CONFIG, "dc_cache_open: %d query heads over %d key/value heads: need a whole ratio of 1 to 64, at most 1024 heads", cfg->n_heads, cfg->n_kv_heads);
+  if (cfg->n_sessions < 1 || cfg->n_sink < 0 || cfg->window < 1 || cfg->ring_rows < cfg->window || cfg->ring_rows > INT_MAX - 4096 - cfg->n_sink)
+    DC_REFUSE(DC_ERR_CONFIG, "dc_cache_open: need n_sessions >= 1, n_sink >= 0, 1 <= window <= ring_rows");
+  if (((double)cfg->n_sink + cfg->ring_rows) * cfg->n_kv_heads * cfg->n_sessions >= 2147483648.0)
+    DC_REFUSE(DC_ERR_CONFIG, "dc_cache_open: the cache has 2^31 rows or more (sessions x key/value heads x rows)");
+  if (dc::misaligned(k_dev) || dc::misaligned(v_dev)) DC_REFUSE(DC_ERR_ARG, "dc_cache_open: k_dev and v_dev must be 16-byte aligned");
+  dc_cache* c = new (std::nothrow) dc_cache();
+  if (!c) DC_REFUSE(DC_ERR_OOM, "dc_cache_open: out of host memory");
+  c->d = dc::CacheDims{cfg->n_sessions, cfg->n_heads, cfg->n_kv_heads, cfg->n_sink, cfg->window, cfg->ring_rows};
+  c->head_dim = cfg->head_dim;
+  c->dtype = cfg->dtype;
+  c->k = k_dev;
+  c->v = v_dev;
+  c->err = nullptr;
+  int major = 0;
+  cudaError_t e = cudaGetDevice(&c->device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, c->device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->n_sm, cudaDevAttrMultiProcessorCount, c->device);
+  if (e == cudaSuccess && major != 10) {
+    delete c;
+    DC_REFUSE(DC_ERR_CUDA, "dc_cache_open: this library is built for sm_100a only");
+  }
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim), cudaFuncAttributeMaxDynamicSharedMemorySize, dc::STEP_SMEM);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)chunk_smem_bytes(c->head_dim));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess && !(cache_map(&c->kmap, c, k_dev) && cache_map(&c->vmap, c, v_dev))) {
+    delete c;
+    DC_REFUSE(DC_ERR_CUDA, "dc_cache_open: cuTensorMapEncodeTiled failed or is unavailable");
+  }
+  if (e == cudaSuccess) e = dc::dev_alloc(&c->err, sizeof(int));
+  if (e == cudaSuccess) e = cudaMemset(c->err, 0, sizeof(int));
+  if (e != cudaSuccess) {
+    dc::dev_free(c->err);
+    delete c;
+    DC_REFUSE(e == cudaErrorMemoryAllocation ? DC_ERR_OOM : DC_ERR_CUDA, "dc_cache_open: %s", cudaGetErrorString(e));
+  }
+  *out = c;
+  return DC_OK;
+}
+
+extern "C" dc_status dc_cache_close(dc_cache* c) {
+  if (!c) DC_REFUSE(DC_ERR_ARG, "dc_cache_close: null pointer argument");
+  dc::dev_free(c->err);     // (waits for the device: no call of this cache is in flight behind it)
+  delete c;
+  return DC_OK;
+}
+
+extern "C" dc_status dc_cache_check(dc_cache* c) {
+  if (!c) DC_REFUSE(DC_ERR_ARG, "dc_cache_check: null pointer argument");
+  int word = 0;
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e == cudaSuccess) e = cudaMemcpy(&word, c->err, sizeof(int), cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && word) e = cudaMemset(c->err, 0, sizeof(int));
+  if (e != cudaSuccess) DC_REFUSE(DC_ERR_CUDA, "dc_cache_check: %s", cudaGetErrorString(e));
+  if (word) DC_REFUSE(DC_ERR_TIMEOUT, "dc_cache_check: a bounded device-side wait of an attention call gave up; its outputs are not valid");
+  return DC_OK;
+}
+
+extern "C" dc_status dc_cache_append(dc_cache* c, const dc_token_batch* b, const dc_qk_norm* nm, const void* qkv_dev, long long qkv_stride, void* q_dev,
+                                     long long q_stride, void* cuda_stream) {
+  const char* who = "dc_cache_append";
+  dc_status st = admit_batch(c, b, who);
+  if (st != DC_OK) return st;
+  if (!nm) DC_REFUSE(DC_ERR_ARG, "%s: null pointer argument", who);
+  if (nm->size != sizeof(dc_qk_norm)) DC_REFUSE(DC_ERR_ARG, "%s: dc_qk_norm.size is %u, this library's is %zu", who, nm->size, sizeof(dc_qk_norm));
+  if (!nm->q_gain_dev || !nm->k_gain_dev || dc::misaligned(nm->q_gain_dev) || dc::misaligned(nm->k_gain_dev))
+    DC_REFUSE(DC_ERR_ARG, "%s: q_gain_dev and k_gain_dev must be 16-byte aligned device pointers", who);
+  if (nm->rot_dim < 0 || nm->rot_dim > c->head_dim || nm->rot_dim % 16 || (nm->rot_dim && !nm->inv_freq_dev))
+    DC_REFUSE(DC_ERR_ARG, "%s: rot_dim is %d: a multiple of 16 up to head_dim, with inv_freq_dev", who, nm->rot_dim);
+  if (!(nm->eps >= 0.f)) DC_REFUSE(DC_ERR_ARG, "%s: eps must not be negative", who);
+  const int D = c->head_dim;
+  if (bad_rows(qkv_dev, qkv_stride, (long long)(c->d.n_heads + 2 * c->d.n_kv_heads) * D) || bad_rows(q_dev, q_stride, (long long)c->d.n_heads * D))
+    DC_REFUSE(DC_ERR_ARG, "%s: qkv_dev and q_dev must be 16-byte aligned, their row strides multiples of 8 values and no shorter than a row", who);
+  if (q_dev == qkv_dev && q_stride != qkv_stride) DC_REFUSE(DC_ERR_ARG, "%s: queries written in place keep the rows' stride", who);
+  const dc::AppendArgs a{c->d, kernel_batch(b), qkv_dev, qkv_stride, q_stride, q_dev, c->k, c->v, nm->q_gain_dev, nm->k_gain_dev, nm->inv_freq_dev, nm->rot_dim, nm->eps};
+  const int chunks = (c->d.n_heads + 2 * c->d.n_kv_heads) * D / 8;
+  const int threads = chunks >= dc::APPEND_THREADS ? dc::APPEND_THREADS : chunks <= 64 ? 64 : (chunks + 31) / 32 * 32;
+  return launched(dc::launch(append_fn(c->dtype, D, nm->interleaved != 0), dim3(b->n_tokens), threads, 0, 1, (cudaStream_t)cuda_stream, &a), who);
+}
+
+extern "C" dc_status dc_cache_attend(dc_cache* c, const dc_token_batch* b, const void* q_dev, long long q_stride, float scale, void* out_dev,
+                                     long long out_stride, void* cuda_stream) {
+  const char* who = "dc_cache_attend";
+  dc_status st = admit_batch(c, b, who);
+  if (st != DC_OK) return st;
+  if (!(scale > 0.f) || isinf(scale)) DC_REFUSE(DC_ERR_ARG, "%s: scale must be positive and finite", who);
+  const int D = c->head_dim;
+  const long long width = (long long)c->d.n_heads * D;
+  if (bad_rows(q_dev, q_stride, width) || bad_rows(out_dev, out_stride, width))
+    DC_REFUSE(DC_ERR_ARG, "%s: q_dev and out_dev must be 16-byte aligned, their row strides multiples of 8 values and no shorter than a row", who);
+  dc::AttendArgs a{c->d, kernel_batch(b), q_dev, c->k, c->v, out_dev, q_stride, out_stride, scale * 1.4426950408889634f, c->d.n_heads / c->d.n_kv_heads, 1, c->err};
+  const long long seen = (long long)c->d.n_sink + c->d.window;     // most rows that a token sees
+  if (b->max_tokens > 1) {
+    dc::ChunkArgs ca{a, 0, c->kmap, c->vmap};
+    const int per = dc::CH_M / a.group;
+    ca.tiles = (b->max_tokens + per - 1) / per;
+    const long long tiles = (long long)ca.tiles * c->d.n_kv_heads * b->n_seqs, steps = (seen + per) / dc::CH_N + 1;
+    // Splits of a tile's rows over a cluster: while all CTAs are resident (two per SM) and each has two steps or more.
+    while (ca.a.splits < 16 && tiles * ca.a.splits * 2 <= 2ll * c->n_sm && ca.a.splits * 4 <= steps) ca.a.splits *= 2;
+    if ((long long)ca.tiles * ca.a.splits > INT_MAX) DC_REFUSE(DC_ERR_ARG, "%s: too many tokens", who);
+    return launched(dc::launch(chunk_fn(c->dtype, D), dim3(ca.tiles * ca.a.splits, c->d.n_kv_heads, b->n_seqs), dc::CH_THREADS, chunk_smem_bytes(D), ca.a.splits,
+                               (cudaStream_t)cuda_stream, &ca), who);
+  }
+  const int groups = (a.group + dc::STEP_ROWS - 1) / dc::STEP_ROWS;
+  // Splits: as many CTAs as two waves' worth of SMs hold, while every warp has a unit of its own.
+  const long long units = seen * D * 2 / dc::STEP_HALF + 1, pairs = (long long)b->n_seqs * c->d.n_kv_heads * groups;
+  while (a.splits < 16 && pairs * a.splits * 2 <= 2ll * c->n_sm && (long long)a.splits * 2 * dc::STEP_WARPS <= units) a.splits *= 2;
+  return launched(dc::launch(step_fn(c->dtype, D), dim3(a.splits, c->d.n_kv_heads * groups, b->n_seqs), dc::STEP_WARPS * 32, dc::STEP_SMEM, a.splits,
+                             (cudaStream_t)cuda_stream, &a), who);
+}
