@@ -498,6 +498,29 @@ dc_status dc_cache_append(dc_cache* cache, const dc_token_batch* batch, const dc
 dc_status dc_cache_attend(dc_cache* cache, const dc_token_batch* batch, const void* q_dev, long long q_stride, float scale,
                           void* out_dev, long long out_stride, void* cuda_stream);
 
+/* The next token of every row of logits.
+ *   z_i = (l_i - max l) / temperature, w_i = exp(z_i), in the order of descending l, ties by lowest index, kept are in turn
+ *     top-k : the first top_k tokens                                           (top_k < 1: all)
+ *     top-p : the shortest beginning of those whose mass reaches top_p times the mass that top-k left, one token at least   (top_p >= 1: all)
+ *     min-p : those of them with w_i >= min_p                                  (min_p <= 0: all)
+ *   token = the first kept index, in the vocabulary's order, whose running mass exceeds u times the kept mass (u >= 1: the last kept one).
+ * temperature <= 0 (or NaN): the lowest index of the largest logit.  NaN logits count as -infinity, which is never chosen; a row without
+ * any other has token -1, probability 0; +infinity outweighs everything finite.  Weights are held in fp64 and their masses as
+ * exact multiples of 2^-45 of the largest weight: the result depends on nothing but the row.
+ *   logits_dev : [n_rows] rows of vocab logits (DC_F32, DC_BF16 or DC_F16), row_stride >= vocab values apart, 16-byte aligned (the rows behind the
+ *                first need not be); u_dev: [n_rows], uniform in [0, 1) - the caller's random numbers
+ *   tokens_dev : [n_rows]; probs_dev: [n_rows] or NULL: the token's share of the kept mass */
+#define DC_SAMPLE_MAX_VOCAB 262144
+typedef struct dc_sample_rules {
+  uint32_t       size;           /* sizeof(dc_sample_rules)                                      */
+  const float*   temperature_dev;   /* each [n_rows], or NULL: 1, 0, 1, 0                         */
+  const int32_t* top_k_dev;
+  const float*   top_p_dev;
+  const float*   min_p_dev;
+} dc_sample_rules;
+dc_status dc_sample_tokens(const void* logits_dev, int dtype, int n_rows, int vocab, long long row_stride, const dc_sample_rules* rules,
+                           const float* u_dev, int32_t* tokens_dev, float* probs_dev, void* cuda_stream);
+
 const char* dc_status_str(dc_status s);
 
 /* Text of the last CUDA or validation error on the calling thread ("" if none). */

@@ -24,7 +24,7 @@ EXPORTS = ["dc_weights_count", "dc_create", "dc_destroy", "dc_stream_open", "dc_
            "dc_decode_batch_host", "dc_profile_begin", "dc_profile_end", "dc_conv_stack_noalloc",
            "dc_selftest_bounded_wait", "dc_stream_snapshot", "dc_stream_restore", "dc_snapshot_free",
            "dc_decode_wavefront", "dc_decode_wavefront_batch", "dc_stream_check_guards", "dc_test_fail_allocation", "dc_test_wavefront_form", "dc_measure_fp32_peak",
-           "dc_cache_open", "dc_cache_close", "dc_cache_check", "dc_cache_append", "dc_cache_attend"]
+           "dc_cache_open", "dc_cache_close", "dc_cache_check", "dc_cache_append", "dc_cache_attend", "dc_sample_tokens"]
 
 
 class dc_config(C.Structure):
@@ -54,6 +54,10 @@ class dc_token_batch(C.Structure):
 class dc_qk_norm(C.Structure):
     _fields_ = [("size", C.c_uint32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float),
                 ("q_gain_dev", C.c_void_p), ("k_gain_dev", C.c_void_p), ("inv_freq_dev", C.c_void_p)]
+
+
+class dc_sample_rules(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("temperature_dev", C.c_void_p), ("top_k_dev", C.c_void_p), ("top_p_dev", C.c_void_p), ("min_p_dev", C.c_void_p)]
 
 
 class DCError(RuntimeError):
@@ -101,6 +105,7 @@ def load_library():
     lib.dc_test_wavefront_form.argtypes = [vp, cp(C.c_int), cp(C.c_uint64)]
     lib.dc_measure_fp32_peak.argtypes = [cp(C.c_double)]
     lib.dc_stream_carry_info.argtypes = [vp, cp(C.c_uint64), C.c_int, cp(C.c_int)]
+    lib.dc_sample_tokens.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.c_longlong, cp(dc_sample_rules), vp, vp, vp, vp]
     lib.dc_get_counters.argtypes = [vp, cp(C.c_uint64)]
     lib.dc_cache_open.argtypes = [cp(dc_cache_config), vp, vp, cp(vp)]
     lib.dc_cache_close.argtypes = [vp]
@@ -534,6 +539,25 @@ class TokenCache:
             self.close()
         except Exception:      # (the interpreter, or the context, is going)
             pass
+
+
+def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=None, stream=None):
+    """dc_sample_tokens: the next token of every row of logits [rows, vocab] (float32, bfloat16 or float16, rows any stride apart) from the random numbers
+    u [rows] in [0, 1).  The rules are CUDA vectors [rows] (float32; top_k int32) or None: off.  Returns the tokens (int32 [rows], in `tokens` if given);
+    probs, if given, receives each token's share of the kept mass."""
+    import torch
+    if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits: CUDA rows [rows, vocab] are wanted, not {tuple(logits.shape)}")
+    n, vocab = logits.shape
+    f32, i32, dev = torch.float32, torch.int32, logits.device
+    if tokens is None:
+        tokens = torch.empty(n, dtype=i32, device=dev)
+    r = dc_sample_rules(C.sizeof(dc_sample_rules), _vector("temperature", temperature, f32, n, dev), _vector("top_k", top_k, i32, n, dev),
+                        _vector("top_p", top_p, f32, n, dev), _vector("min_p", min_p, f32, n, dev))
+    _check(load_library().dc_sample_tokens(logits.data_ptr(), _dtype_code(logits), n, vocab, logits.stride(0) if n > 1 else max(logits.stride(0), vocab), C.byref(r),
+                                           _vector("u", u, f32, n, dev), _vector("tokens", tokens, i32, n, dev), _vector("probs", probs, f32, n, dev),
+                                           _token_stream(stream, dev)), "dc_sample_tokens")
+    return tokens
 
 
 def _on(device):

@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdc.so")
-SOURCES = ["dc_api.cu", "dc_f32_kernels.cu", "dc_flow.cu", "dc_token_cache.cu"]
+SOURCES = ["dc_api.cu", "dc_f32_kernels.cu", "dc_flow.cu", "dc_token_cache.cu", "dc_sample.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared"]
 

@@ -125,3 +125,12 @@ def test_null_and_misaligned_caches_are_refused():
     assert lib.dc_cache_close(None) == 1 and lib.dc_cache_check(None) == 1
     assert lib.dc_cache_append(None, None, None, None, 0, None, 0, None) == 1
     assert lib.dc_cache_attend(None, None, None, 0, 1.0, None, 0, None) == 1
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=3), dict(n_rows=0), dict(n_rows=65536), dict(vocab=0), dict(vocab=262145, stride=262145), dict(stride=99), dict(logits=0x10004), dict(logits=None),
+                                dict(u=None), dict(tokens=None), dict(size=4)])
+def test_samples_outside_of_the_kernel_are_refused(kw):
+    a = {**dict(dtype=0, n_rows=2, vocab=100, stride=100, logits=0x10000, u=0x20000, tokens=0x30000, size=C.sizeof(binding.dc_sample_rules)), **kw}
+    r = binding.dc_sample_rules(a["size"])
+    st = dc.load_library().dc_sample_tokens(a["logits"], a["dtype"], a["n_rows"], a["vocab"], a["stride"], C.byref(r), a["u"], a["tokens"], None, None)
+    assert binding.STATUS[st] == "DC_ERR_ARG" and dc.load_library().dc_last_error()
