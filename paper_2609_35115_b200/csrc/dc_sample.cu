@@ -2,8 +2,7 @@
 //
 // One pass over the logits: a cluster of CTAs keeps a row in shared memory, each CTA a contiguous slice of the vocabulary, and
 // everything after the load happens there.  The rules cut a prefix of the order "descending logit, ties by lowest index", so the kept set is
-// a cut key and a number of its ties; cuts are found by radix selection on the logits' order-preserving bits, 11 bits at a time, by
-// counts (top-k) or by mass (top-p).
+// a cut key and a number of its ties; cuts are found by selection through histograms, by counts (top-k) or by mass (top-p).
 //
 // The result is a whole number that has to be the right one, so masses are exact: a weight exp((l - max) / T) is evaluated in fp64
 // (2^(j/256) from a table times a polynomial; about 2^-50) and held as an integer multiple of 2^-45.  Integer sums do not depend on their order: atomics, splits
@@ -40,7 +39,8 @@ struct SampleShared {
   unsigned long long hist[2][SMP_BINS];
   double             table[256];           // 2^(j / 256)
   unsigned long long best;                 // key and inverted index of the slice's maximum
-  unsigned long long total, kept;          // mass of the slice that top-k left; mass that all rules left
+  unsigned long long range[2];             // smallest and largest key of a selection's last bin
+  unsigned long long kept;                 // mass of the slice's kept tokens
   unsigned long long warp_sum[SMP_WARPS];
   unsigned long long above;                // count or mass above the found bin, and of it
   unsigned long long inside;
@@ -115,6 +115,7 @@ template <typename T>
 __device__ __forceinline__ void load_slice(const T* src, int n, int shift, float* l) {
   constexpr int VE = 16 / sizeof(T);
   const int vectors = (shift + n + VE - 1) / VE;
+#pragma unroll 4
   for (int v = threadIdx.x; v < vectors; v += SMP_THREADS) {
     const int at = v * VE - shift;
     alignas(16) T x[VE];
@@ -137,82 +138,173 @@ __device__ __forceinline__ void load_slice(const T* src, int n, int shift, float
   }
 }
 
-// Radix selection over the cluster: the key at which the running count (BY_MASS: mass) of the descending order reaches `target`, among
-// the keys above `floor_key`; what lies above it; and what it holds itself.  False if the whole of it does not reach the target.
-// `buf` alternates: a buffer is cleared two rounds after it was filled, when every CTA has read it.
-template <bool BY_MASS, bool COARSE>
-__device__ bool radix_select(SampleShared& sh, const float* l, int places, const Weigh& w, uint32_t floor_key, unsigned long long target, int splits, int& buf, uint32_t* key,
-                             unsigned long long* above, unsigned long long* inside) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  uint32_t prefix = 0;
-  unsigned long long over = 0;
-  // logits of 16-bit types have nothing in their keys' lowest 10 bits but the sign's copy
-  for (int level = 0; level < (COARSE ? 2 : 3); ++level) {
-    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-    for (int i = tid; i < SMP_BINS; i += SMP_THREADS) sh.hist[buf][i] = 0;
-    if (tid == 0) sh.bin = -1;
-    __syncthreads();
-    for (int i = tid * 4; i < places; i += SMP_THREADS * 4) {
-      const float4 v = *reinterpret_cast<const float4*>(l + i);
-      const float x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t k = key_of(x[e]);
-        if (k > floor_key && (level == 0 || k >> (shift + bits) == prefix)) {
-          const uint32_t b = k >> shift & ((1u << bits) - 1);
-          if (BY_MASS) {
-            const unsigned long long m = w.fixed(x[e]);
-            if (m) atomicAdd(&sh.hist[buf][b], m);
-          } else {
-            atomicAdd(reinterpret_cast<uint32_t*>(&sh.hist[buf][b]), 1u);
-          }
-        }
-      }
-    }
-    if (splits > 1) {
-      ptx::cluster_arrive();
-      ptx::cluster_wait();
-    } else {
-      __syncthreads();
-    }
-    // bins from the highest down, SMP_PER of them a thread
-    unsigned long long own[SMP_PER], sum = 0;
-    const int b0 = SMP_BINS - 1 - tid * SMP_PER;
-#pragma unroll
-    for (int i = 0; i < SMP_PER; ++i) own[i] = 0;
-    for (int c = 0; c < splits; ++c) {
-      const uint32_t at = ptx::map_to_cta(ptx::smem_u32(&sh.hist[buf][b0 - (SMP_PER - 1)]), c);
-#pragma unroll
-      for (int i = 0; i < SMP_PER; ++i) own[i] += ld_cluster64(at + (SMP_PER - 1 - i) * 8);
-    }
-#pragma unroll
-    for (int i = 0; i < SMP_PER; ++i) sum += own[i];
-    unsigned long long upto = warp_scan(sum, lane);
-    if (lane == 31) sh.warp_sum[warp] = upto;
-    __syncthreads();
-    upto -= sum;
-    for (int i = 0; i < warp; ++i) upto += sh.warp_sum[i];
-    upto += over;
-#pragma unroll
-    for (int i = 0; i < SMP_PER; ++i) {
-      if (upto < target && upto + own[i] >= target) {
-        sh.bin = b0 - i;
-        sh.above = upto;
-        sh.inside = own[i];
-      }
-      upto += own[i];
-    }
-    __syncthreads();
-    buf ^= 1;
-    if (sh.bin < 0) return false;      // (level 0 only)
-    prefix = prefix << bits | (uint32_t)sh.bin;
-    over = sh.above;
-    *inside = sh.inside;
+__device__ __forceinline__ void cluster_or_block_sync(int splits) {
+  if (splits > 1) {
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  } else {
     __syncthreads();
   }
-  if (COARSE) prefix = prefix << 10 | (prefix >> 21 ? 0u : 0x3ffu);
+}
+
+// Bins of a row.  Selection needs bins that fall with the logit and spread the row's logits, so that few of a warp's lanes meet in one:
+// 32 to a factor of two of weight, then 2048 in each of those, by fp32 arithmetic (each operation is monotone, and the
+// second bin is exact in what the first one left).
+struct Binned {
+  float top, scale;      // scale: 64 log2(e) / T, of half a difference (a whole one may pass fp32's range)
+  static __device__ __forceinline__ bool is_weighed(float t) { return t < 46.f * 32.f; }    // behind that a weight is below half of 2^-45
+  // (rounded products and differences, spelt out: joined into one operation they would not be what the bins were cut by)
+  __device__ __forceinline__ float place(float l) const { return l == top ? 0.f : __fmul_rn(fmaf(l, -0.5f, 0.5f * top), scale); }
+  static __device__ __forceinline__ int inner(float t, int bin) { return (int)__fmul_rn(__fsub_rn(t, (float)bin), 2048.f); }
+};
+
+// What a selection sums: one for every logit, or its mass.
+template <bool BY_MASS>
+__device__ __forceinline__ void add_to_bin(unsigned long long* bin, const Weigh& w, float l) {
+  uint32_t* half = reinterpret_cast<uint32_t*>(bin);
+  if (!BY_MASS) {
+    atomicAdd(half, 1u);
+    return;
+  }
+  // 32-bit adds, with the carry: shared memory adds those in place, 64-bit ones in a loop
+  const unsigned long long m = w.fixed(l);
+  const uint32_t lo = (uint32_t)m, old = atomicAdd(half, lo), hi = (uint32_t)(m >> 32) + (old + lo < lo);
+  if (hi) atomicAdd(half + 1, hi);
+}
+
+// Sums the cluster's histograms from bin 0 up (DOWN: from the last bin down) and finds the bin in which `over` plus the running sum reaches
+// target(total).
+template <bool DOWN, typename F>
+__device__ __forceinline__ bool find_bin(SampleShared& sh, int buf, unsigned long long over, F target_of, int splits, int* bin, unsigned long long* above, unsigned long long* inside) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) sh.bin = -1;
+  cluster_or_block_sync(splits);
+  unsigned long long own[SMP_PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < SMP_PER; ++i) own[i] = 0;
+  const int b0 = DOWN ? SMP_BINS - SMP_PER - tid * SMP_PER : tid * SMP_PER;
+  for (int c = 0; c < splits; ++c) {
+    const uint32_t at = ptx::map_to_cta(ptx::smem_u32(&sh.hist[buf][b0]), c);
+#pragma unroll
+    for (int i = 0; i < SMP_PER; ++i) own[i] += ld_cluster64(at + (DOWN ? SMP_PER - 1 - i : i) * 8);
+  }
+#pragma unroll
+  for (int i = 0; i < SMP_PER; ++i) sum += own[i];
+  unsigned long long upto = warp_scan(sum, lane);
+  if (lane == 31) sh.warp_sum[warp] = upto;
+  __syncthreads();
+  upto += over - sum;
+  unsigned long long total = 0;
+#pragma unroll
+  for (int i = 0; i < SMP_WARPS; ++i) {
+    if (i < warp) upto += sh.warp_sum[i];
+    total += sh.warp_sum[i];
+  }
+  const unsigned long long target = target_of(total);
+#pragma unroll
+  for (int i = 0; i < SMP_PER; ++i) {
+    if (upto < target && upto + own[i] >= target) {
+      sh.bin = DOWN ? b0 + SMP_PER - 1 - i : b0 + i;
+      sh.above = upto;
+      sh.inside = own[i];
+    }
+    upto += own[i];
+  }
+  __syncthreads();
+  *bin = sh.bin;
+  *above = sh.above;
+  *inside = sh.inside;
+  __syncthreads();      // (the next search begins by resetting them)
+  return *bin >= 0;
+}
+
+// Calls f(logit) for every logit of this thread's share of the slice.
+template <typename F>
+__device__ __forceinline__ void each_logit(const float* l, int places, F f) {
+  for (int i = threadIdx.x * 4; i < places; i += SMP_THREADS * 4) {
+    const float4 v = *reinterpret_cast<const float4*>(l + i);
+    f(v.x);
+    f(v.y);
+    f(v.z);
+    f(v.w);
+  }
+}
+
+// Selection over the cluster: the key at which the running count (BY_MASS: mass) of the descending order reaches the target, among the
+// keys above `floor_key`; what lies above it; and what it holds itself.  False if the whole of it does not reach the target.  `buf` alternates: a buffer is cleared
+// two rounds after it was filled, when every CTA has read it.
+template <bool BY_MASS, typename F>
+__device__ __forceinline__ bool select(SampleShared& sh, const float* l, int places, const Weigh& w, const Binned& bins, uint32_t floor_key, F target_of, int splits, int& buf, uint32_t* key,
+                                       unsigned long long* above, unsigned long long* inside) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int b0, b1;
+  auto clear = [&] {
+    for (int i = tid; i < SMP_BINS; i += SMP_THREADS) sh.hist[buf][i] = 0;
+    __syncthreads();
+  };
+  clear();
+  each_logit(l, places, [&](float x) {
+    const float t = bins.place(x);
+    if (Binned::is_weighed(t) && key_of(x) > floor_key) add_to_bin<BY_MASS>(&sh.hist[buf][(int)t], w, x);
+  });
+  unsigned long long target = 0;
+  const bool found = find_bin<false>(sh, buf, 0, [&](unsigned long long total) { return target = target_of(total); }, splits, &b0, above, inside);
+  buf ^= 1;
+  if (!found) return false;
+  auto known = [&](unsigned long long) { return target; };
+  clear();
+  each_logit(l, places, [&](float x) {
+    const float t = bins.place(x);
+    if (Binned::is_weighed(t) && (int)t == b0 && key_of(x) > floor_key) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
+  });
+  find_bin<false>(sh, buf, *above, known, splits, &b1, above, inside);
+  buf ^= 1;
+  auto in_bin = [&](float x) {
+    const float t = bins.place(x);
+    return Binned::is_weighed(t) && (int)t == b0 && Binned::inner(t, b0) == b1 && key_of(x) > floor_key;
+  };
+  // one logit, as a rule, or equal ones: the bin's smallest and largest key (the latter inverted)
+  uint32_t lo = 0xffffffffu, hi = 0xffffffffu;
+  each_logit(l, places, [&](float x) {
+    if (in_bin(x)) {
+      lo = min(lo, key_of(x));
+      hi = min(hi, ~key_of(x));
+    }
+  });
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_min_sync(0xffffffffu, hi);
+  if (lane == 0) sh.warp_sum[warp] = (unsigned long long)hi << 32 | lo;
+  __syncthreads();
+  for (int i = 0; i < SMP_WARPS; ++i) {
+    lo = min(lo, (uint32_t)sh.warp_sum[i]);
+    hi = min(hi, (uint32_t)(sh.warp_sum[i] >> 32));
+  }
+  if (splits > 1) {
+    if (tid == 0) sh.range[BY_MASS] = (unsigned long long)hi << 32 | lo;
+    cluster_or_block_sync(splits);
+    for (int c = 0; c < splits; ++c) {
+      const unsigned long long x = ld_cluster64(ptx::map_to_cta(ptx::smem_u32(&sh.range[BY_MASS]), c));
+      lo = min(lo, (uint32_t)x);
+      hi = min(hi, (uint32_t)(x >> 32));
+    }
+  }
+  *key = lo;
+  if (lo == ~hi) return true;
+  // several logits share the bin (scores far closer to each other than a weight can tell): by the bits of their keys
+  uint32_t prefix = 0;
+  for (int level = 0; level < 3; ++level) {
+    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+    clear();
+    each_logit(l, places, [&](float x) {
+      const uint32_t k = key_of(x);
+      if (in_bin(x) && (level == 0 || k >> (shift + bits) == prefix)) add_to_bin<BY_MASS>(&sh.hist[buf][k >> shift & ((1u << bits) - 1)], w, x);
+    });
+    int digit;
+    find_bin<true>(sh, buf, *above, known, splits, &digit, above, inside);
+    buf ^= 1;
+    prefix = prefix << bits | (uint32_t)digit;
+  }
   *key = prefix;
-  *above = over;
   return true;
 }
 
@@ -222,7 +314,6 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   __shared__ SampleShared sh;
   ptx::pdl_wait();
   ptx::pdl_launch();
-  constexpr bool COARSE = sizeof(T) == 2;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x, row = blockIdx.y;
   const int from = min(a.vocab, rank * a.slice), n = min(a.vocab, from + a.slice) - from;
   const T* src = static_cast<const T*>(a.logits) + (long long)row * a.stride + from;
@@ -284,47 +375,29 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   // ---- the cut ---------------------------------------------------------------------------------------------------------------
   const float top = logit_of(best_key);
   const Weigh w{1.4426950408889634074 / (double)temperature, (double)top, isinf(top) != 0, sh.table};
+  const Binned bins{top, isinf(top) ? 1e30f : fminf((float)(64.0 * w.scale), 1e30f)};
   Cut cut{KEY_NONE, 0};
   int buf = 0;
   uint32_t key;
   unsigned long long above, inside;
-  if (top_k > 0 && top_k < a.vocab && radix_select<false, COARSE>(sh, l, places, w, KEY_NONE, (unsigned long long)top_k, a.splits, buf, &key, &above, &inside)) {
+  if (top_k > 0 && top_k < a.vocab && select<false>(sh, l, places, w, bins, KEY_NONE, [&](unsigned long long) { return (unsigned long long)top_k; }, a.splits, buf, &key, &above, &inside)) {
     cut.key = key;
     cut.ties = top_k - above;
     if (cut.ties == inside) cut = Cut{key - 1, 0};      // (all of them)
   }
-  unsigned long long mass = 0;      // of the kept tokens, where it is known
   if (top_p < 1.f) {
-    // the mass that top-k left: the keys above the cut, and the cut's ties
-    unsigned long long sum = 0;
-    for (int i = tid * 4; i < places; i += SMP_THREADS * 4) {
-      const float4 v = *reinterpret_cast<const float4*>(l + i);
-      const float x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (key_of(x[e]) > cut.key) sum += w.fixed(x[e]);
-    }
-    sum = warp_sum(sum);
-    __syncthreads();
-    if (lane == 0) sh.warp_sum[warp] = sum;
-    __syncthreads();
-    if (tid == 0) {
-      sum = 0;
-      for (int i = 0; i < SMP_WARPS; ++i) sum += sh.warp_sum[i];
-      sh.total = sum;
-    }
-    if (a.splits > 1) {
-      ptx::cluster_arrive();
-      ptx::cluster_wait();
-    } else {
-      __syncthreads();
-    }
-    for (int c = 0; c < a.splits; ++c) mass += ld_cluster64(ptx::map_to_cta(ptx::smem_u32(&sh.total), c));
-    if (cut.ties) mass += cut.ties * w.fixed(logit_of(cut.key));
-    const double want = ceil((double)top_p * (double)mass);
-    const unsigned long long target = want >= 1.0 ? (unsigned long long)want : 1ull;
-    if (radix_select<true, COARSE>(sh, l, places, w, cut.ties ? cut.key - 1 : cut.key, target < mass ? target : mass, a.splits, buf, &key, &above, &inside)) {
-      const unsigned long long each = w.fixed(logit_of(key)), need = (target < mass ? target : mass) - above;
+    // of the mass that top-k left: the keys above the cut and the cut's ties (the bins hold all of those)
+    const uint32_t floor_key = cut.ties ? cut.key - 1 : cut.key;
+    const unsigned long long too_many = cut.ties ? (inside - cut.ties) * w.fixed(logit_of(cut.key)) : 0;
+    unsigned long long target = 0;
+    auto part_of = [&](unsigned long long total) {
+      const unsigned long long mass = total - too_many;
+      const double want = ceil((double)top_p * (double)mass);
+      target = want >= 1.0 ? (unsigned long long)want : 1ull;
+      return target = target < mass ? target : mass;
+    };
+    if (select<true>(sh, l, places, w, bins, floor_key, part_of, a.splits, buf, &key, &above, &inside)) {
+      const unsigned long long each = w.fixed(logit_of(key)), need = target - above;
       cut.key = key;
       cut.ties = (need + each - 1) / each;
       if (cut.ties * each == inside) cut = Cut{key - 1, 0};
@@ -398,7 +471,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     if (i < warp) start += sh.warp_sum[i];
     total += sh.warp_sum[i];
   }
-  mass = total;
+  unsigned long long mass = total;
   if (a.splits > 1) {
     if (tid == 0) sh.kept = total;
     ptx::cluster_arrive();

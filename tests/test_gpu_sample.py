@@ -220,3 +220,17 @@ def test_shares_of_many_draws(dc):
     u = (torch.arange(n, device="cuda") + 0.5) / n
     got = torch.bincount(dc.sample_tokens(row.repeat(n, 1), u).long(), minlength=vocab).double()
     assert (got - n * torch.softmax(row.double(), 0)).abs().max() <= 1.0 + n * 2.0 ** -24      # (u is rounded to fp32)
+
+
+@pytest.mark.parametrize("T", [1e30, 1e38, 3e4, 50.0])
+def test_scores_closer_than_weights_can_tell(dc, T):
+    """High temperatures: neighbouring logits have equal weights, and their order still decides who is kept."""
+    rng = np.random.default_rng(17)
+    n, vocab = 6, 9001
+    u = rng.random(n)
+    l = torch.tensor(rng.standard_normal((n, vocab)), dtype=torch.float32, device="cuda")
+    check(dc, l, u, T=np.full(n, T), k=1 + np.arange(n) * 1700)
+    check(dc, l, u, T=np.full(n, T), p=(np.arange(n) + 0.5) / n)
+    l[:, ::3] *= 1e38
+    l[0, 7], l[0, 8] = torch.finfo(torch.float32).max, torch.finfo(torch.float32).min
+    check(dc, l, u, T=np.full(n, T), k=1 + np.arange(n) * 1700, p=np.full(n, 0.8))
