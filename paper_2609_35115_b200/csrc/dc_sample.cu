@@ -19,7 +19,7 @@ namespace dc {
 namespace {
 
 constexpr int SMP_THREADS = 512, SMP_WARPS = SMP_THREADS / 32;
-constexpr int SMP_BINS = 2048, SMP_PER = SMP_BINS / SMP_THREADS;
+constexpr int SMP_BINS = 2048;
 constexpr int SMP_SLICE = 16384;          // logits of a CTA at most
 constexpr int SMP_MAX_CLUSTER = 16;
 constexpr uint32_t KEY_NONE = 0x007fffffu;   // key of -infinity: such logits, and NaN, take no part
@@ -35,17 +35,19 @@ struct SampleArgs {
   float*         probs;
 };
 
+constexpr int SMP_GROUPS = SMP_BINS / 32;
+
 struct SampleShared {
   unsigned long long hist[2][SMP_BINS];
-  double             table[256];           // 2^(j / 256)
-  unsigned long long best;                 // key and inverted index of the slice's maximum
-  unsigned long long range[2];             // smallest and largest key of a selection's last bin
-  unsigned long long kept;                 // mass of the slice's kept tokens
+  unsigned long long group[2][SMP_GROUPS];   // sums of 32 neighbouring bins
+  double             table[256];             // 2^(j / 256)
+  unsigned long long best;                   // the slice's maximum: key and inverted index
+  unsigned long long range[2];               // smallest and inverted largest key of a selection's last bin
+  unsigned long long kept;                   // mass of the slice's kept tokens
   unsigned long long warp_sum[SMP_WARPS];
-  unsigned long long above;                // count or mass above the found bin, and of it
-  unsigned long long inside;
+  unsigned long long above, inside, target;  // of the found bin
   uint32_t           warp_ties[SMP_WARPS];
-  uint32_t           ties;                 // of the slice
+  uint32_t           ties;                   // of the slice
   int                bin;
 };
 
@@ -64,6 +66,22 @@ __device__ __forceinline__ uint32_t ld_cluster32(uint32_t addr) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
+// Sum of a word over the cluster's CTAs.
+__device__ __forceinline__ unsigned long long cluster_sum(const unsigned long long* word, int splits) {
+  const uint32_t at = ptx::smem_u32(word);
+  unsigned long long s = 0;
+#pragma unroll 8
+  for (int c = 0; c < splits; ++c) s += ld_cluster64(ptx::map_to_cta(at, c));
+  return s;
+}
+__device__ __forceinline__ void cluster_or_block_sync(int splits) {
+  if (splits > 1) {
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  } else {
+    __syncthreads();
+  }
+}
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
 #pragma unroll
   for (int m = 16; m; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
@@ -78,16 +96,14 @@ __device__ __forceinline__ unsigned long long warp_scan(unsigned long long v, in
   return v;
 }
 
-// Weights of a row.
+// Weights of a row: 2^((l - top) scale), of logits whose exponent is at least `least` (which is -46 or more: what lies below is under half of 2^-45).
 struct Weigh {
-  double scale, top;   // log2(e) / T, the largest logit
-  bool   infinite;     // the largest logit is +infinity: it alone has weight
+  double scale, top, least;   // scale: log2(e) / T
   const double* table;
-  // 2^y for -46 <= y <= 0: y = k / 256 + f with |f| <= 2^-9, 2^f by the first terms of its series (the rest is below 2^-54)
+  // y = k / 256 + f with |f| <= 2^-9; 2^f by the first terms of its series (the rest is below 2^-54)
   __device__ __forceinline__ double value(float l) const {
-    if (infinite) return l == INFINITY ? 1.0 : 0.0;
     const double y = ((double)l - top) * scale;
-    if (!(y >= -46.0)) return 0.0;
+    if (!(y >= least)) return 0.0;
     const double magic = 6755399441055744.0 / 256.0;      // 1.5 * 2^52 / 256
     const double t = y + magic, f = y - (t - magic);
     const int k = __double2loint(t);
@@ -96,25 +112,29 @@ struct Weigh {
     const double v = fma(r, p, r);
     return __hiloint2double(__double2hiint(v) + (k >> 8) * (1 << 20), __double2loint(v));
   }
-  // in units of 2^-45: the lowest bit of a number just above 2^7 is that
-  static __device__ __forceinline__ unsigned long long fix(double w) { return (unsigned long long)(__double_as_longlong(w + 128.0) - __double_as_longlong(128.0)); }
+  // in units of 2^-45: the lowest bit of a number just above 2^7 is that.  raw() counts RAW_ZERO too many, which a sum takes off once.
+  static constexpr unsigned long long RAW_ZERO = 0x4060000000000000ull;      // 128.0
+  static __device__ __forceinline__ unsigned long long raw(double w) { return (unsigned long long)__double_as_longlong(w + 128.0); }
+  static __device__ __forceinline__ unsigned long long fix(double w) { return raw(w) - RAW_ZERO; }
   __device__ __forceinline__ unsigned long long fixed(float l) const { return fix(value(l)); }
 };
 
-// The kept tokens: keys above `key`, and the first `ties` (in the vocabulary's order) of those equal to it.
+// The kept tokens: logits from `low` up, and the first `ties` (in the vocabulary's order) of those equal to `tie`, just below.
 struct Cut {
-  uint32_t           key;
+  float              low, tie;
   unsigned long long ties;
 };
 
-// Loads the slice: 16-byte vectors on their own alignment, so that the first `shift` places of shared memory lie before the slice.
 template <typename T>
 __device__ __forceinline__ float as_float(T x) { return (float)x; }
 
+// Loads the slice into shared memory and returns this thread's maximum.  16-byte vectors on their own alignment: the first
+// `shift` places of shared memory lie before the slice.
 template <typename T>
-__device__ __forceinline__ void load_slice(const T* src, int n, int shift, float* l) {
+__device__ __forceinline__ float load_slice(const T* src, int n, int shift, float* l) {
   constexpr int VE = 16 / sizeof(T);
   const int vectors = (shift + n + VE - 1) / VE;
+  float top = -INFINITY;
 #pragma unroll 4
   for (int v = threadIdx.x; v < vectors; v += SMP_THREADS) {
     const int at = v * VE - shift;
@@ -130,31 +150,36 @@ __device__ __forceinline__ void load_slice(const T* src, int n, int shift, float
       float y[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float f = as_float(x[i + e]) + 0.0f;      // (-0 becomes 0: the two are one logit)
-        y[e] = f == f ? f : -INFINITY;
+        y[e] = fmaxf(as_float(x[i + e]), -INFINITY) + 0.0f;      // (NaN becomes -infinity, -0 becomes 0: the two zeros are one logit)
+        top = fmaxf(top, y[e]);
       }
       *reinterpret_cast<float4*>(l + v * VE + i) = make_float4(y[0], y[1], y[2], y[3]);
     }
   }
+  return top;
 }
 
-__device__ __forceinline__ void cluster_or_block_sync(int splits) {
-  if (splits > 1) {
-    ptx::cluster_arrive();
-    ptx::cluster_wait();
-  } else {
-    __syncthreads();
+// Calls f(logit) for every logit of this thread's share of the slice.
+template <typename F>
+__device__ __forceinline__ void each_logit(const float* l, int places, F f) {
+#pragma unroll 2
+  for (int i = threadIdx.x * 4; i < places; i += SMP_THREADS * 4) {
+    const float4 v = *reinterpret_cast<const float4*>(l + i);
+    f(v.x);
+    f(v.y);
+    f(v.z);
+    f(v.w);
   }
 }
 
 // Bins of a row.  Selection needs bins that fall with the logit and spread the row's logits, so that few of a warp's lanes meet in one:
 // 32 to a factor of two of weight, then 2048 in each of those, by fp32 arithmetic (each operation is monotone, and the
-// second bin is exact in what the first one left).
+// second bin is exact in what the first one left; products and differences are spelt out, joined into one operation they would not be what
+// the bins were cut by).
 struct Binned {
-  float top, scale;      // scale: 64 log2(e) / T, of half a difference (a whole one may pass fp32's range)
-  static __device__ __forceinline__ bool is_weighed(float t) { return t < 46.f * 32.f; }    // behind that a weight is below half of 2^-45
-  // (rounded products and differences, spelt out: joined into one operation they would not be what the bins were cut by)
-  __device__ __forceinline__ float place(float l) const { return l == top ? 0.f : __fmul_rn(fmaf(l, -0.5f, 0.5f * top), scale); }
+  float half_top, scale;      // scale: 64 log2(e) / T, of half a difference (a whole one may pass fp32's range)
+  static __device__ __forceinline__ bool is_weighed(float t) { return t < 46.f * 32.f; }
+  __device__ __forceinline__ float place(float l) const { return __fmul_rn(fmaf(l, -0.5f, half_top), scale); }
   static __device__ __forceinline__ int inner(float t, int bin) { return (int)__fmul_rn(__fsub_rn(t, (float)bin), 2048.f); }
 };
 
@@ -172,72 +197,64 @@ __device__ __forceinline__ void add_to_bin(unsigned long long* bin, const Weigh&
   if (hi) atomicAdd(half + 1, hi);
 }
 
-// Sums the cluster's histograms from bin 0 up (DOWN: from the last bin down) and finds the bin in which `over` plus the running sum reaches
-// target(total).
+// Finds the bin of the cluster's histograms in which `over` plus the running sum, from bin 0 up (DOWN: from the last bin down), reaches
+// target(total): groups of bins first, then the group's bins, so that little is read from the other CTAs.
 template <bool DOWN, typename F>
-__device__ __forceinline__ bool find_bin(SampleShared& sh, int buf, unsigned long long over, F target_of, int splits, int* bin, unsigned long long* above, unsigned long long* inside) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) sh.bin = -1;
+__device__ __forceinline__ bool find_bin(SampleShared& sh, int buf, unsigned long long over, F target_of, int splits) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncthreads();
+#pragma unroll
+  for (int g = warp * (SMP_GROUPS / SMP_WARPS); g < (warp + 1) * (SMP_GROUPS / SMP_WARPS); ++g) {
+    const unsigned long long s = warp_sum(sh.hist[buf][g * 32 + lane]);
+    if (lane == 0) sh.group[buf][g] = s;
+  }
   cluster_or_block_sync(splits);
-  unsigned long long own[SMP_PER], sum = 0;
+  if (warp == 0) {
+    unsigned long long s[SMP_GROUPS / 32], sum = 0;
 #pragma unroll
-  for (int i = 0; i < SMP_PER; ++i) own[i] = 0;
-  const int b0 = DOWN ? SMP_BINS - SMP_PER - tid * SMP_PER : tid * SMP_PER;
-  for (int c = 0; c < splits; ++c) {
-    const uint32_t at = ptx::map_to_cta(ptx::smem_u32(&sh.hist[buf][b0]), c);
-#pragma unroll
-    for (int i = 0; i < SMP_PER; ++i) own[i] += ld_cluster64(at + (DOWN ? SMP_PER - 1 - i : i) * 8);
-  }
-#pragma unroll
-  for (int i = 0; i < SMP_PER; ++i) sum += own[i];
-  unsigned long long upto = warp_scan(sum, lane);
-  if (lane == 31) sh.warp_sum[warp] = upto;
-  __syncthreads();
-  upto += over - sum;
-  unsigned long long total = 0;
-#pragma unroll
-  for (int i = 0; i < SMP_WARPS; ++i) {
-    if (i < warp) upto += sh.warp_sum[i];
-    total += sh.warp_sum[i];
-  }
-  const unsigned long long target = target_of(total);
-#pragma unroll
-  for (int i = 0; i < SMP_PER; ++i) {
-    if (upto < target && upto + own[i] >= target) {
-      sh.bin = DOWN ? b0 + SMP_PER - 1 - i : b0 + i;
-      sh.above = upto;
-      sh.inside = own[i];
+    for (int i = 0; i < SMP_GROUPS / 32; ++i) {
+      const int g = lane * (SMP_GROUPS / 32) + i;
+      s[i] = cluster_sum(&sh.group[buf][DOWN ? SMP_GROUPS - 1 - g : g], splits);
+      sum += s[i];
     }
-    upto += own[i];
+    unsigned long long upto = warp_scan(sum, lane);
+    const unsigned long long target = target_of(__shfl_sync(0xffffffffu, upto, 31));
+    upto += over - sum;
+    int group = -1;
+    unsigned long long base = 0;
+#pragma unroll
+    for (int i = 0; i < SMP_GROUPS / 32; ++i) {
+      if (upto < target && upto + s[i] >= target) {
+        group = lane * (SMP_GROUPS / 32) + i;
+        base = upto;
+      }
+      upto += s[i];
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, group >= 0);
+    if (lane == 0) sh.bin = -1;
+    if (who) {
+      group = __shfl_sync(0xffffffffu, group, __ffs(who) - 1);
+      base = __shfl_sync(0xffffffffu, base, __ffs(who) - 1);
+      const int at = group * 32 + lane, bin = DOWN ? SMP_BINS - 1 - at : at;
+      const unsigned long long own = cluster_sum(&sh.hist[buf][bin], splits), before = warp_scan(own, lane) + base - own;
+      if (before < target && before + own >= target) {
+        sh.bin = bin;
+        sh.above = before;
+        sh.inside = own;
+        sh.target = target;
+      }
+    }
   }
   __syncthreads();
-  *bin = sh.bin;
-  *above = sh.above;
-  *inside = sh.inside;
-  __syncthreads();      // (the next search begins by resetting them)
-  return *bin >= 0;
-}
-
-// Calls f(logit) for every logit of this thread's share of the slice.
-template <typename F>
-__device__ __forceinline__ void each_logit(const float* l, int places, F f) {
-  for (int i = threadIdx.x * 4; i < places; i += SMP_THREADS * 4) {
-    const float4 v = *reinterpret_cast<const float4*>(l + i);
-    f(v.x);
-    f(v.y);
-    f(v.z);
-    f(v.w);
-  }
+  return sh.bin >= 0;      // (all of this is written anew behind a barrier that everyone passes)
 }
 
 // Selection over the cluster: the key at which the running count (BY_MASS: mass) of the descending order reaches the target, among the
-// keys above `floor_key`; what lies above it; and what it holds itself.  False if the whole of it does not reach the target.  `buf` alternates: a buffer is cleared
-// two rounds after it was filled, when every CTA has read it.
+// logits from `low` up; what lies above it, what it holds itself, and the target are left in `sh`.  False if the whole of it does not
+// reach the target.  `buf` alternates: a buffer is cleared two rounds after it was filled, when every CTA has read it.
 template <bool BY_MASS, typename F>
-__device__ __forceinline__ bool select(SampleShared& sh, const float* l, int places, const Weigh& w, const Binned& bins, uint32_t floor_key, F target_of, int splits, int& buf, uint32_t* key,
-                                       unsigned long long* above, unsigned long long* inside) {
+__device__ __forceinline__ bool select(SampleShared& sh, const float* l, int places, const Weigh& w, const Binned& bins, float low, F target_of, int splits, int& buf, uint32_t* key) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int b0, b1;
   auto clear = [&] {
     for (int i = tid; i < SMP_BINS; i += SMP_THREADS) sh.hist[buf][i] = 0;
     __syncthreads();
@@ -245,23 +262,26 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   clear();
   each_logit(l, places, [&](float x) {
     const float t = bins.place(x);
-    if (Binned::is_weighed(t) && key_of(x) > floor_key) add_to_bin<BY_MASS>(&sh.hist[buf][(int)t], w, x);
+    if (Binned::is_weighed(t) && x >= low) add_to_bin<BY_MASS>(&sh.hist[buf][(int)t], w, x);
   });
-  unsigned long long target = 0;
-  const bool found = find_bin<false>(sh, buf, 0, [&](unsigned long long total) { return target = target_of(total); }, splits, &b0, above, inside);
+  const bool found = find_bin<false>(sh, buf, 0, target_of, splits);
   buf ^= 1;
   if (!found) return false;
+  const int b0 = sh.bin;
+  const unsigned long long target = sh.target;
   auto known = [&](unsigned long long) { return target; };
+  unsigned long long above = sh.above;
   clear();
   each_logit(l, places, [&](float x) {
     const float t = bins.place(x);
-    if (Binned::is_weighed(t) && (int)t == b0 && key_of(x) > floor_key) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
+    if (Binned::is_weighed(t) && (int)t == b0 && x >= low) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
   });
-  find_bin<false>(sh, buf, *above, known, splits, &b1, above, inside);
+  find_bin<false>(sh, buf, above, known, splits);
   buf ^= 1;
+  const int b1 = sh.bin;
   auto in_bin = [&](float x) {
     const float t = bins.place(x);
-    return Binned::is_weighed(t) && (int)t == b0 && Binned::inner(t, b0) == b1 && key_of(x) > floor_key;
+    return Binned::is_weighed(t) && (int)t == b0 && Binned::inner(t, b0) == b1 && x >= low;
   };
   // one logit, as a rule, or equal ones: the bin's smallest and largest key (the latter inverted)
   uint32_t lo = 0xffffffffu, hi = 0xffffffffu;
@@ -290,19 +310,20 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   }
   *key = lo;
   if (lo == ~hi) return true;
-  // several logits share the bin (scores far closer to each other than a weight can tell): by the bits of their keys
+  // several logits share the bin (scores far closer to each other than weights can tell): by the bits of their keys
   uint32_t prefix = 0;
+#pragma unroll 1
   for (int level = 0; level < 3; ++level) {
     const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+    above = sh.above;
     clear();
     each_logit(l, places, [&](float x) {
       const uint32_t k = key_of(x);
       if (in_bin(x) && (level == 0 || k >> (shift + bits) == prefix)) add_to_bin<BY_MASS>(&sh.hist[buf][k >> shift & ((1u << bits) - 1)], w, x);
     });
-    int digit;
-    find_bin<true>(sh, buf, *above, known, splits, &digit, above, inside);
+    find_bin<true>(sh, buf, above, known, splits);
     buf ^= 1;
-    prefix = prefix << bits | (uint32_t)digit;
+    prefix = prefix << bits | (uint32_t)sh.bin;
   }
   *key = prefix;
   return true;
@@ -322,38 +343,40 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   const int top_k = a.top_k ? a.top_k[row] : 0;
   const bool greedy = !(temperature > 0.f) || top_k == 1;
 
-  load_slice(src, n, shift, l);
+  float top = load_slice(src, n, shift, l);
   if (!greedy && tid < 256) sh.table[tid] = exp2(tid * (1.0 / 256.0));
   // a warp's part of the slice is contiguous: what is summed in the vocabulary's order is summed by warps, in steps of 128
-  constexpr int STEP = 128;
-  const int filled = (shift + n + 7) & ~7;                                  // (vectors of 16 bytes fill up to 8 places)
+  constexpr int STEP = 128, VE = 16 / sizeof(T);
+  const int filled = (shift + n + VE - 1) / VE * VE;
   const int part = (filled + SMP_WARPS * STEP - 1) / (SMP_WARPS * STEP) * STEP, places = part * SMP_WARPS;
-  for (int i = ((shift + n + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T))) * (16 / (int)sizeof(T)) + tid; i < places; i += SMP_THREADS) l[i] = -INFINITY;
-  __syncthreads();
+  for (int i = filled + tid; i < places; i += SMP_THREADS) l[i] = -INFINITY;
 
-  // ---- the largest logit and its first place ------------------------------------------------------------------------------
-  unsigned long long best = 0;
-  for (int i = tid * 4; i < places; i += SMP_THREADS * 4) {
-    const float4 v = *reinterpret_cast<const float4*>(l + i);
-    const float x[4] = {v.x, v.y, v.z, v.w};
+  // ---- the largest logit -----------------------------------------------------------------------------------------------------
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const unsigned long long k = (unsigned long long)key_of(x[e]) << 32 | (uint32_t)~(from - shift + i + e);
-      best = k > best ? k : best;
-    }
-  }
-#pragma unroll
-  for (int m = 16; m; m >>= 1) {
-    const unsigned long long x = __shfl_xor_sync(0xffffffffu, best, m);
-    best = x > best ? x : best;
-  }
-  if (lane == 0) sh.warp_sum[warp] = best;
+  for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+  if (lane == 0) sh.warp_sum[warp] = __float_as_uint(top);
   __syncthreads();
-  for (int i = 0; i < SMP_WARPS; ++i) best = sh.warp_sum[i] > best ? sh.warp_sum[i] : best;
+#pragma unroll
+  for (int i = 0; i < SMP_WARPS; ++i) top = fmaxf(top, __uint_as_float((uint32_t)sh.warp_sum[i]));
+  unsigned long long best = (unsigned long long)key_of(top) << 32;
+  if (greedy) {      // and its first place
+    uint32_t at = 0xffffffffu;
+    for (int i = tid * 4; i < places; i += SMP_THREADS * 4) {
+      const float4 v = *reinterpret_cast<const float4*>(l + i);
+      const uint32_t e = v.x == top ? 0 : v.y == top ? 1 : v.z == top ? 2 : v.w == top ? 3 : 4;
+      if (e < 4) at = min(at, (uint32_t)(from - shift + i) + e);
+    }
+    at = __reduce_min_sync(0xffffffffu, at);
+    if (lane == 0) sh.warp_ties[warp] = at;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SMP_WARPS; ++i) at = min(at, sh.warp_ties[i]);
+    best |= (uint32_t)~at;
+  }
   if (a.splits > 1) {
     if (tid == 0) sh.best = best;
-    ptx::cluster_arrive();
-    ptx::cluster_wait();
+    cluster_or_block_sync(a.splits);
+#pragma unroll 8
     for (int c = 0; c < a.splits; ++c) {
       const unsigned long long x = ld_cluster64(ptx::map_to_cta(ptx::smem_u32(&sh.best), c));
       best = x > best ? x : best;
@@ -365,44 +388,48 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       a.tokens[row] = best_key <= KEY_NONE ? -1 : (int)~(uint32_t)best;
       if (a.probs) a.probs[row] = best_key <= KEY_NONE ? 0.f : 1.f;
     }
-    if (a.splits > 1) {      // no CTA's shared memory goes while another reads it
-      ptx::cluster_arrive();
-      ptx::cluster_wait();
-    }
+    if (a.splits > 1) cluster_or_block_sync(a.splits);      // no CTA's shared memory goes while another reads it
     return;
+  }
+  top = logit_of(best_key);
+  if (isinf(top)) {      // +infinity outweighs everything finite: as zeros against nothing
+    for (int i = tid; i < places; i += SMP_THREADS) l[i] = l[i] == INFINITY ? 0.f : -INFINITY;
+    top = 0.f;
+    __syncthreads();
   }
 
   // ---- the cut ---------------------------------------------------------------------------------------------------------------
-  const float top = logit_of(best_key);
-  const Weigh w{1.4426950408889634074 / (double)temperature, (double)top, isinf(top) != 0, sh.table};
-  const Binned bins{top, isinf(top) ? 1e30f : fminf((float)(64.0 * w.scale), 1e30f)};
-  Cut cut{KEY_NONE, 0};
+  Weigh w{1.4426950408889634074 / (double)temperature, (double)top, -46.0, sh.table};
+  const Binned bins{0.5f * top, fminf((float)(64.0 * w.scale), 1e30f)};
+  Cut cut{-3.402823466e38f, 0.f, 0};      // every finite logit
+  auto cut_at = [&](uint32_t key, unsigned long long ties, bool all) {
+    cut.ties = all ? 0 : ties;
+    cut.tie = logit_of(key);
+    cut.low = all ? cut.tie : logit_of(key + 1);
+  };
   int buf = 0;
   uint32_t key;
-  unsigned long long above, inside;
-  if (top_k > 0 && top_k < a.vocab && select<false>(sh, l, places, w, bins, KEY_NONE, [&](unsigned long long) { return (unsigned long long)top_k; }, a.splits, buf, &key, &above, &inside)) {
-    cut.key = key;
-    cut.ties = top_k - above;
-    if (cut.ties == inside) cut = Cut{key - 1, 0};      // (all of them)
+  unsigned long long too_many = 0;      // ties that top-k leaves out
+  if (top_k > 0 && top_k < a.vocab && select<false>(sh, l, places, w, bins, cut.low, [&](unsigned long long) { return (unsigned long long)top_k; }, a.splits, buf, &key)) {
+    too_many = sh.inside - (top_k - sh.above);
+    cut_at(key, top_k - sh.above, too_many == 0);
   }
   if (top_p < 1.f) {
-    // of the mass that top-k left: the keys above the cut and the cut's ties (the bins hold all of those)
-    const uint32_t floor_key = cut.ties ? cut.key - 1 : cut.key;
-    const unsigned long long too_many = cut.ties ? (inside - cut.ties) * w.fixed(logit_of(cut.key)) : 0;
-    unsigned long long target = 0;
+    // of the mass that top-k left: the logits above the cut and the cut's ties (the bins hold all of those)
+    if (too_many) too_many *= w.fixed(cut.tie);
     auto part_of = [&](unsigned long long total) {
       const unsigned long long mass = total - too_many;
       const double want = ceil((double)top_p * (double)mass);
-      target = want >= 1.0 ? (unsigned long long)want : 1ull;
-      return target = target < mass ? target : mass;
+      const unsigned long long target = want >= 1.0 ? (unsigned long long)want : 1ull;
+      return target < mass ? target : mass;
     };
-    if (select<true>(sh, l, places, w, bins, floor_key, part_of, a.splits, buf, &key, &above, &inside)) {
-      const unsigned long long each = w.fixed(logit_of(key)), need = target - above;
-      cut.key = key;
-      cut.ties = (need + each - 1) / each;
-      if (cut.ties * each == inside) cut = Cut{key - 1, 0};
+    if (select<true>(sh, l, places, w, bins, cut.ties ? cut.tie : cut.low, part_of, a.splits, buf, &key)) {
+      const unsigned long long each = w.fixed(logit_of(key)), ties = (sh.target - sh.above + each - 1) / each;
+      cut_at(key, ties, ties * each == sh.inside);
     }
   }
+  if (min_p > 0.f) w.least = fmax(w.least, log2((double)min_p));      // (1 and more: 0, the largest logit's)
+  if (w.least > 0.0) w.least = 0.0;
 
   // ---- ties: those of the slices before this one, and of the warps before this one -----------------------------------------------
   unsigned long long ties_before = 0;
@@ -410,7 +437,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     uint32_t mine = 0;
     for (int i = warp * part + lane * 4; i < (warp + 1) * part; i += STEP) {
       const float4 v = *reinterpret_cast<const float4*>(l + i);
-      mine += (key_of(v.x) == cut.key) + (key_of(v.y) == cut.key) + (key_of(v.z) == cut.key) + (key_of(v.w) == cut.key);
+      mine += (v.x == cut.tie) + (v.y == cut.tie) + (v.z == cut.tie) + (v.w == cut.tie);
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0) sh.warp_ties[warp] = mine;
@@ -421,37 +448,39 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       sh.ties = all;
     }
     if (a.splits > 1) {
-      ptx::cluster_arrive();
-      ptx::cluster_wait();
+      cluster_or_block_sync(a.splits);
       for (int c = 0; c < rank; ++c) ties_before += ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.ties), c));
     }
     for (int i = 0; i < warp; ++i) ties_before += sh.warp_ties[i];
   }
-  // The fixed weights of four neighbouring places, of kept tokens only; `seen`: the cut's ties in front of this step.
+  // The raw weights of four neighbouring places, of kept tokens only; `seen`: the cut's ties in front of this step.
   auto weights = [&](int i, unsigned long long& seen, unsigned long long* m) {
     const float4 v = *reinterpret_cast<const float4*>(l + i);
     const float x[4] = {v.x, v.y, v.z, v.w};
-    unsigned long long rank4 = 0;
+    bool on[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) on[e] = x[e] >= cut.low;
     if (cut.ties) {
       uint32_t eq = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) eq += key_of(x[e]) == cut.key;
+      for (int e = 0; e < 4; ++e) eq += x[e] == cut.tie;
       uint32_t upto = eq;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
         const uint32_t y = __shfl_up_sync(0xffffffffu, upto, d);
         if (lane >= d) upto += y;
       }
-      rank4 = seen + upto - eq;
+      unsigned long long rank4 = seen + upto - eq;
       seen += __shfl_sync(0xffffffffu, upto, 31);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (x[e] == cut.tie) on[e] = rank4++ < cut.ties;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t k = key_of(x[e]);
-      bool on = k > cut.key;
-      if (k == cut.key && cut.ties) on = rank4++ < cut.ties;
-      const double wd = on ? w.value(x[e]) : 0.0;
-      m[e] = on && wd >= (double)min_p ? Weigh::fix(wd) : 0;
+    for (int e = 0; e < 4; ++e) m[e] = Weigh::RAW_ZERO;
+    if (on[0] || on[1] || on[2] || on[3]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = Weigh::raw(on[e] ? w.value(x[e]) : 0.0);
     }
   };
 
@@ -460,23 +489,24 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   for (int i = warp * part + lane * 4; i < (warp + 1) * part; i += STEP) {
     unsigned long long m[4];
     weights(i, seen, m);
-    sum += m[0] + m[1] + m[2] + m[3];
+    sum += (m[0] + m[1]) + (m[2] + m[3]);
   }
+  sum -= (unsigned long long)(part / 32) * Weigh::RAW_ZERO;
   sum = warp_sum(sum);
   __syncthreads();
   if (lane == 0) sh.warp_sum[warp] = sum;
   __syncthreads();
-  unsigned long long start = 0, total = 0;
+  unsigned long long start = 0, mass = 0;
+#pragma unroll
   for (int i = 0; i < SMP_WARPS; ++i) {
     if (i < warp) start += sh.warp_sum[i];
-    total += sh.warp_sum[i];
+    mass += sh.warp_sum[i];
   }
-  unsigned long long mass = total;
   if (a.splits > 1) {
-    if (tid == 0) sh.kept = total;
-    ptx::cluster_arrive();
-    ptx::cluster_wait();
+    if (tid == 0) sh.kept = mass;
+    cluster_or_block_sync(a.splits);
     mass = 0;
+#pragma unroll 8
     for (int c = 0; c < a.splits; ++c) {
       const unsigned long long x = ld_cluster64(ptx::map_to_cta(ptx::smem_u32(&sh.kept), c));
       if (c < rank) start += x;
@@ -492,11 +522,12 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     for (int i = warp * part + lane * 4; i < (warp + 1) * part; i += STEP) {
       unsigned long long m[4];
       weights(i, seen, m);
-      const unsigned long long four = m[0] + m[1] + m[2] + m[3], upto = warp_scan(four, lane) + run;
-      unsigned long long before = upto - four;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] -= Weigh::RAW_ZERO;
+      const unsigned long long four = m[0] + m[1] + m[2] + m[3], upto = warp_scan(four, lane) + run, before = upto - four;
       if (target >= before && target < upto) {
-        int e = 0;
-        while (target >= before + m[e]) before += m[e++];
+        const unsigned long long in = target - before;
+        const int e = in < m[0] ? 0 : in < m[0] + m[1] ? 1 : in < m[0] + m[1] + m[2] ? 2 : 3;
         a.tokens[row] = from - shift + i + e;
         if (a.probs) a.probs[row] = (float)(w.value(l[i + e]) / ((double)mass / (double)ONE));
       }
@@ -504,10 +535,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       if (target < run) break;
     }
   }
-  if (a.splits > 1) {
-    ptx::cluster_arrive();
-    ptx::cluster_wait();
-  }
+  if (a.splits > 1) cluster_or_block_sync(a.splits);
 }
 
 template <typename T>
