@@ -18,12 +18,13 @@
 namespace dc {
 namespace {
 
-constexpr int SMP_THREADS = 512, SMP_WARPS = SMP_THREADS / 32;
-constexpr int SMP_BINS = 2048;
-constexpr int SMP_SLICE = 16384;          // logits of a CTA at most
+constexpr int SMP_THREADS = 256, SMP_WARPS = SMP_THREADS / 32;
+constexpr int SMP_BINS = 1024;
+constexpr int SMP_SLICE = 8192;           // logits of a CTA, while 16 CTAs are enough (then up to twice as many)
 constexpr int SMP_MAX_CLUSTER = 16;
 constexpr uint32_t KEY_NONE = 0x007fffffu;   // key of -infinity: such logits, and NaN, take no part
 constexpr unsigned long long ONE = 1ull << 45;
+constexpr float LOWEST = -3.402823466e38f;
 
 struct SampleArgs {
   const void*    logits;
@@ -40,7 +41,7 @@ constexpr int SMP_GROUPS = SMP_BINS / 32;
 struct SampleShared {
   unsigned long long hist[2][SMP_BINS];
   unsigned long long group[2][SMP_GROUPS];   // sums of 32 neighbouring bins
-  double             table[256];             // 2^(j / 256)
+  double             table[256];             // 2^(j / 256): one a thread
   unsigned long long best;                   // the slice's maximum: key and inverted index
   unsigned long long range[2];               // smallest and inverted largest key of a selection's last bin
   unsigned long long kept;                   // mass of the slice's kept tokens
@@ -51,8 +52,9 @@ struct SampleShared {
   int                bin;
 };
 
+// Bits in the logits' order (the two zeros are one logit).
 __device__ __forceinline__ uint32_t key_of(float l) {
-  const uint32_t b = __float_as_uint(l);
+  const uint32_t b = __float_as_uint(l + 0.0f);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float logit_of(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
@@ -96,14 +98,27 @@ __device__ __forceinline__ unsigned long long warp_scan(unsigned long long v, in
   return v;
 }
 
-// Weights of a row: 2^((l - top) scale), of logits whose exponent is at least `least` (which is -46 or more: what lies below is under half of 2^-45).
+// 2^(j / 256), j = 0 .. 255, by the series of exp(j ln 2 / 256), which 24 terms take below the last bit.
+struct Exp2Table {
+  double v[256];
+  constexpr Exp2Table() : v() {
+    for (int j = 0; j < 256; ++j) {
+      const double x = j * (0.69314718055994530942 / 256.0);
+      double sum = 0.0;
+      for (int k = 24; k >= 1; --k) sum = (sum + 1.0) * x / k;      // x + x^2 / 2 + ..., smallest terms first
+      v[j] = 1.0 + sum;
+    }
+  }
+};
+__device__ constexpr Exp2Table exp2_table;
+
+// Weights of a row: 2^((l - top) scale).
 struct Weigh {
-  double scale, top, least;   // scale: log2(e) / T
+  double scale, top;     // scale: log2(e) / T
   const double* table;
-  // y = k / 256 + f with |f| <= 2^-9; 2^f by the first terms of its series (the rest is below 2^-54)
+  // y = k / 256 + f with |f| <= 2^-9; 2^f by the first terms of its series (the rest is below 2^-54).  Of finite l whose y is -64 or more.
   __device__ __forceinline__ double value(float l) const {
     const double y = ((double)l - top) * scale;
-    if (!(y >= least)) return 0.0;
     const double magic = 6755399441055744.0 / 256.0;      // 1.5 * 2^52 / 256
     const double t = y + magic, f = y - (t - magic);
     const int k = __double2loint(t);
@@ -112,10 +127,8 @@ struct Weigh {
     const double v = fma(r, p, r);
     return __hiloint2double(__double2hiint(v) + (k >> 8) * (1 << 20), __double2loint(v));
   }
-  // in units of 2^-45: the lowest bit of a number just above 2^7 is that.  raw() counts RAW_ZERO too many, which a sum takes off once.
-  static constexpr unsigned long long RAW_ZERO = 0x4060000000000000ull;      // 128.0
-  static __device__ __forceinline__ unsigned long long raw(double w) { return (unsigned long long)__double_as_longlong(w + 128.0); }
-  static __device__ __forceinline__ unsigned long long fix(double w) { return raw(w) - RAW_ZERO; }
+  // in units of 2^-45: the lowest bit of a number just above 2^7 is that
+  static __device__ __forceinline__ unsigned long long fix(double w) { return (unsigned long long)__double_as_longlong(w + 128.0) - 0x4060000000000000ull; }
   __device__ __forceinline__ unsigned long long fixed(float l) const { return fix(value(l)); }
 };
 
@@ -129,7 +142,7 @@ template <typename T>
 __device__ __forceinline__ float as_float(T x) { return (float)x; }
 
 // Loads the slice into shared memory and returns this thread's maximum.  16-byte vectors on their own alignment: the first
-// `shift` places of shared memory lie before the slice.
+// `shift` places of shared memory lie before the slice.  (NaN is left: it compares as false, like -infinity it is never kept.)
 template <typename T>
 __device__ __forceinline__ float load_slice(const T* src, int n, int shift, float* l) {
   constexpr int VE = 16 / sizeof(T);
@@ -147,13 +160,9 @@ __device__ __forceinline__ float load_slice(const T* src, int n, int shift, floa
     }
 #pragma unroll
     for (int i = 0; i < VE; i += 4) {
-      float y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y[e] = fmaxf(as_float(x[i + e]), -INFINITY) + 0.0f;      // (NaN becomes -infinity, -0 becomes 0: the two zeros are one logit)
-        top = fmaxf(top, y[e]);
-      }
-      *reinterpret_cast<float4*>(l + v * VE + i) = make_float4(y[0], y[1], y[2], y[3]);
+      const float4 y = make_float4(as_float(x[i]), as_float(x[i + 1]), as_float(x[i + 2]), as_float(x[i + 3]));
+      top = fmaxf(fmaxf(top, fmaxf(y.x, y.y)), fmaxf(y.z, y.w));
+      *reinterpret_cast<float4*>(l + v * VE + i) = y;
     }
   }
   return top;
@@ -173,14 +182,15 @@ __device__ __forceinline__ void each_logit(const float* l, int places, F f) {
 }
 
 // Bins of a row.  Selection needs bins that fall with the logit and spread the row's logits, so that few of a warp's lanes meet in one:
-// 32 to a factor of two of weight, then 2048 in each of those, by fp32 arithmetic (each operation is monotone, and the
+// 22 to a factor of two of weight, then 1024 in each of those, by fp32 arithmetic (each operation is monotone, and the
 // second bin is exact in what the first one left; products and differences are spelt out, joined into one operation they would not be what
 // the bins were cut by).
 struct Binned {
-  float half_top, scale;      // scale: 64 log2(e) / T, of half a difference (a whole one may pass fp32's range)
-  static __device__ __forceinline__ bool is_weighed(float t) { return t < 46.f * 32.f; }
+  float half_top, scale;      // scale: 44 log2(e) / T, of half a difference (a whole one may pass fp32's range)
+  static constexpr float END = 46.f * 22.f;      // 2^-46: what lies behind rounds to nothing
   __device__ __forceinline__ float place(float l) const { return __fmul_rn(fmaf(l, -0.5f, half_top), scale); }
-  static __device__ __forceinline__ int inner(float t, int bin) { return (int)__fmul_rn(__fsub_rn(t, (float)bin), 2048.f); }
+  __device__ __forceinline__ float logit(float t) const { return 2.f * (half_top - t / scale); }
+  static __device__ __forceinline__ int inner(float t, int bin) { return (int)__fmul_rn(__fsub_rn(t, (float)bin), (float)SMP_BINS); }
 };
 
 // What a selection sums: one for every logit, or its mass.
@@ -262,7 +272,7 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   clear();
   each_logit(l, places, [&](float x) {
     const float t = bins.place(x);
-    if (Binned::is_weighed(t) && x >= low) add_to_bin<BY_MASS>(&sh.hist[buf][(int)t], w, x);
+    if (x >= low) add_to_bin<BY_MASS>(&sh.hist[buf][(int)t], w, x);
   });
   const bool found = find_bin<false>(sh, buf, 0, target_of, splits);
   buf ^= 1;
@@ -271,17 +281,24 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   const unsigned long long target = sh.target;
   auto known = [&](unsigned long long) { return target; };
   unsigned long long above = sh.above;
+  // the bin's logits lie in this range (half a bin and two steps wider than that on both sides), which is cheaper to ask for
+  const float x_top = 2.f * bins.half_top;
+  float x_lo = fmaxf(low, bins.logit(b0 + 1.5f)), x_hi = fminf(x_top, bins.logit(b0 - 0.5f));
+  if (x_lo > low) x_lo = logit_of(key_of(x_lo) - 2);
+  if (x_hi < x_top) x_hi = logit_of(key_of(x_hi) + 2);
   clear();
   each_logit(l, places, [&](float x) {
+    if (!(x >= x_lo && x <= x_hi)) return;
     const float t = bins.place(x);
-    if (Binned::is_weighed(t) && (int)t == b0 && x >= low) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
+    if (x >= low && (int)t == b0) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
   });
   find_bin<false>(sh, buf, above, known, splits);
   buf ^= 1;
   const int b1 = sh.bin;
   auto in_bin = [&](float x) {
+    if (!(x >= x_lo && x <= x_hi)) return false;
     const float t = bins.place(x);
-    return Binned::is_weighed(t) && (int)t == b0 && Binned::inner(t, b0) == b1 && x >= low;
+    return x >= low && (int)t == b0 && Binned::inner(t, b0) == b1;
   };
   // one logit, as a rule, or equal ones: the bin's smallest and largest key (the latter inverted)
   uint32_t lo = 0xffffffffu, hi = 0xffffffffu;
@@ -313,8 +330,8 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   // several logits share the bin (scores far closer to each other than weights can tell): by the bits of their keys
   uint32_t prefix = 0;
 #pragma unroll 1
-  for (int level = 0; level < 3; ++level) {
-    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+  for (int level = 0; level < 4; ++level) {
+    const int shift = 22 - 10 * level > 0 ? 22 - 10 * level : 0, bits = level == 3 ? 2 : 10;
     above = sh.above;
     clear();
     each_logit(l, places, [&](float x) {
@@ -330,7 +347,7 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
 }
 
 template <typename T>
-__global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs a) {
   extern __shared__ __align__(16) float l[];
   __shared__ SampleShared sh;
   ptx::pdl_wait();
@@ -344,7 +361,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   const bool greedy = !(temperature > 0.f) || top_k == 1;
 
   float top = load_slice(src, n, shift, l);
-  if (!greedy && tid < 256) sh.table[tid] = exp2(tid * (1.0 / 256.0));
+  sh.table[tid] = exp2_table.v[tid];
   // a warp's part of the slice is contiguous: what is summed in the vocabulary's order is summed by warps, in steps of 128
   constexpr int STEP = 128, VE = 16 / sizeof(T);
   const int filled = (shift + n + VE - 1) / VE * VE;
@@ -399,9 +416,13 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   }
 
   // ---- the cut ---------------------------------------------------------------------------------------------------------------
-  Weigh w{1.4426950408889634074 / (double)temperature, (double)top, -46.0, sh.table};
-  const Binned bins{0.5f * top, fminf((float)(64.0 * w.scale), 1e30f)};
-  Cut cut{-3.402823466e38f, 0.f, 0};      // every finite logit
+  const double scale = 1.4426950408889634074 / (double)temperature;
+  const Weigh w{scale, (double)top, sh.table};
+  const Binned bins{0.5f * top, fminf((float)(44.0 * scale), 1e30f)};
+  // the logits that weigh anything: nearly as far down as the bins go (two bins short of it: place() is off by less, but where one step of the
+  // logits passes a bin, and there a few steps up are enough)
+  Cut cut{fmaxf((float)((double)top - 45.9 / scale), LOWEST), 0.f, 0};
+  while (cut.low < top && !(bins.place(cut.low) < Binned::END)) cut.low = logit_of(key_of(cut.low) + 1);
   auto cut_at = [&](uint32_t key, unsigned long long ties, bool all) {
     cut.ties = all ? 0 : ties;
     cut.tie = logit_of(key);
@@ -428,8 +449,23 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       cut_at(key, ties, ties * each == sh.inside);
     }
   }
-  if (min_p > 0.f) w.least = fmax(w.least, log2((double)min_p));      // (1 and more: 0, the largest logit's)
-  if (w.least > 0.0) w.least = 0.0;
+  if (min_p > 0.f) {      // the smallest logit whose weight is min_p or more (1 and more: the largest logit): a step or two from where it should be, else by halves
+    const double least = min_p < 1.f ? log2((double)min_p) : 0.0;
+    const auto enough = [&](uint32_t k) { return ((double)logit_of(k) - (double)top) * scale >= least; };
+    uint32_t hi = key_of(top), lo = key_of(LOWEST);
+    const uint32_t near = key_of(fmaxf(fminf((float)((double)top + least / scale), top), LOWEST));
+    if (near < hi - 2 && enough(near + 2)) hi = near + 2;
+    if (near > lo + 2 && !enough(near - 2)) lo = near - 2;
+    if (enough(lo)) hi = lo;
+    while (hi - lo > 1) {      // (lo: not enough, hi: enough)
+      const uint32_t mid = lo + (hi - lo) / 2;
+      if (enough(mid)) hi = mid;
+      else lo = mid;
+    }
+    const float x = logit_of(hi);
+    if (x > cut.tie) cut.ties = 0;
+    cut.low = fmaxf(cut.low, x);
+  }
 
   // ---- ties: those of the slices before this one, and of the warps before this one -----------------------------------------------
   unsigned long long ties_before = 0;
@@ -453,7 +489,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     }
     for (int i = 0; i < warp; ++i) ties_before += sh.warp_ties[i];
   }
-  // The raw weights of four neighbouring places, of kept tokens only; `seen`: the cut's ties in front of this step.
+  // The weights of four neighbouring places, of kept tokens only; `seen`: the cut's ties in front of this step.
   auto weights = [&](int i, unsigned long long& seen, unsigned long long* m) {
     const float4 v = *reinterpret_cast<const float4*>(l + i);
     const float x[4] = {v.x, v.y, v.z, v.w};
@@ -477,10 +513,13 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
         if (x[e] == cut.tie) on[e] = rank4++ < cut.ties;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) m[e] = Weigh::RAW_ZERO;
-    if (on[0] || on[1] || on[2] || on[3]) {
+    for (int e = 0; e < 4; ++e) m[e] = 0;
+    if (on[0] || on[1] || on[2] || on[3]) {      // (no branch for each: four chains run side by side)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) m[e] = Weigh::raw(on[e] ? w.value(x[e]) : 0.0);
+      for (int e = 0; e < 4; ++e) {
+        const unsigned long long f = w.fixed(x[e]);
+        m[e] = on[e] ? f : 0;
+      }
     }
   };
 
@@ -491,7 +530,6 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     weights(i, seen, m);
     sum += (m[0] + m[1]) + (m[2] + m[3]);
   }
-  sum -= (unsigned long long)(part / 32) * Weigh::RAW_ZERO;
   sum = warp_sum(sum);
   __syncthreads();
   if (lane == 0) sh.warp_sum[warp] = sum;
@@ -522,8 +560,6 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     for (int i = warp * part + lane * 4; i < (warp + 1) * part; i += STEP) {
       unsigned long long m[4];
       weights(i, seen, m);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) m[e] -= Weigh::RAW_ZERO;
       const unsigned long long four = m[0] + m[1] + m[2] + m[3], upto = warp_scan(four, lane) + run, before = upto - four;
       if (target >= before && target < upto) {
         const unsigned long long in = target - before;
@@ -544,7 +580,7 @@ cudaError_t launch_sample(const SampleArgs& a, int rows, size_t smem, cudaStream
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess && ready != dev) {
-    e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (SMP_SLICE + SMP_WARPS * 128 + 64) * 4);
+    e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (SMP_SLICE + SMP_WARPS * 128) * 4);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) ready = dev;
   }
@@ -597,7 +633,7 @@ extern "C" dc_status dc_sample_tokens(const void* logits_dev, int dtype, int n_r
   }
   SampleArgs a{logits_dev, row_stride, vocab, 0, 1, rules->temperature_dev, rules->top_p_dev, rules->min_p_dev, u_dev, rules->top_k_dev, tokens_dev, probs_dev};
   // CTAs of a row: as many as its logits need, and while SMs are idle more, down to 4096 logits each.
-  while ((long long)a.splits * SMP_SLICE < vocab) a.splits *= 2;
+  while (a.splits < SMP_MAX_CLUSTER && (long long)a.splits * SMP_SLICE < vocab) a.splits *= 2;
   while (a.splits < SMP_MAX_CLUSTER && (long long)n_rows * a.splits * 2 <= n_sm && vocab / a.splits > 4096) a.splits *= 2;
   a.slice = ((vocab + a.splits - 1) / a.splits + 7) & ~7;
   const int filled = (a.slice + 7 + 7) & ~7, part = (filled + SMP_WARPS * 128 - 1) / (SMP_WARPS * 128) * 128;
