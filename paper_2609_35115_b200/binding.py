@@ -424,15 +424,13 @@ def _dtype_code(t) -> int:
         raise TypeError(f"{t.dtype} is not served: float32, bfloat16 or float16") from None
 
 
-def _vector(name, t, dtype, n=None, device=None):
-    """Checks a small device array that a call reads; returns its address."""
+def _vector(name, t, dtype, n=None, index=None):
+    """Checks a small device array that a call reads or writes; returns its address (None: none)."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or (t.shape[0] > 1 and t.stride(0) != 1) or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name}: a contiguous CUDA vector of {dtype}" + (f" and {n} values" if n is not None else "") + f" is wanted, not {tuple(t.shape)} {t.dtype}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.dim() == 1 and t.is_contiguous() and t.get_device() == (t.get_device() if index is None else index) and t.is_cuda and (n is None or t.numel() == n):
+        return t.data_ptr()
+    raise ValueError(f"{name}: a contiguous vector of {'' if n is None else f'{n} '}{dtype} on the call's CUDA device is wanted, not {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
 class TokenBatch:
@@ -441,14 +439,14 @@ class TokenBatch:
 
     def __init__(self, sessions, start, cu_tokens=None, n_tokens: Optional[int] = None, max_tokens: int = 1):
         import torch
-        self.device, n = start.device, start.shape[0]
+        self.index, n = start.get_device(), start.shape[0]
         self._kept = (sessions, start, cu_tokens)
         self.c = c = dc_token_batch()
         c.size, c.n_seqs, c.max_tokens = C.sizeof(dc_token_batch), n, max_tokens
         c.n_tokens = n if n_tokens is None else n_tokens
         c.start_dev = _vector("start", start, torch.int32, n)
-        c.sessions_dev = _vector("sessions", sessions, torch.int32, n, start.device)
-        c.cu_tokens_dev = _vector("cu_tokens", cu_tokens, torch.int32, n + 1, start.device)
+        c.sessions_dev = _vector("sessions", sessions, torch.int32, n, self.index)
+        c.cu_tokens_dev = _vector("cu_tokens", cu_tokens, torch.int32, n + 1, self.index)
         self.n_tokens, self.address = c.n_tokens, C.addressof(c)
 
 
@@ -457,14 +455,14 @@ class QKNorm:
 
     def __init__(self, q_gain, k_gain, inv_freq=None, eps: float = 1e-6, interleaved: bool = False):
         import torch
-        self.device, self.head_dim = q_gain.device, q_gain.shape[0]
+        self.index, self.head_dim = q_gain.get_device(), q_gain.shape[0]
         self._kept = (q_gain, k_gain, inv_freq)
         self.c = c = dc_qk_norm()
         c.size, c.eps, c.interleaved = C.sizeof(dc_qk_norm), eps, int(interleaved)
         c.q_gain_dev = _vector("q_gain", q_gain, torch.float32)
-        c.k_gain_dev = _vector("k_gain", k_gain, torch.float32, self.head_dim, self.device)
+        c.k_gain_dev = _vector("k_gain", k_gain, torch.float32, self.head_dim, self.index)
         c.rot_dim = 0 if inv_freq is None else 2 * inv_freq.shape[0]
-        c.inv_freq_dev = _vector("inv_freq", inv_freq, torch.float32, None, self.device)
+        c.inv_freq_dev = _vector("inv_freq", inv_freq, torch.float32, None, self.index)
         self.address = C.addressof(c)
 
 
@@ -477,7 +475,8 @@ class TokenCache:
         for name, t in (("k", k), ("v", v)):
             if not t.is_cuda or t.dim() != 4 or not t.is_contiguous() or t.shape != k.shape or t.dtype != k.dtype or t.device != k.device:
                 raise ValueError(f"{name}: a contiguous CUDA tensor [sessions, kv_heads, rows, head_dim] is wanted, k and v alike")
-        self.lib, self.k, self.v, self.device, self.dtype = load_library(), k, v, k.device, k.dtype
+        self.lib, self.k, self.v, self.device, self.dtype, self._index = load_library(), k, v, k.device, k.dtype, k.get_device()
+        self._append, self._attend = self.lib.dc_cache_append, self.lib.dc_cache_attend
         c = dc_cache_config()
         c.size, c.dtype, c.n_heads, c.n_sink = C.sizeof(dc_cache_config), _dtype_code(k), n_heads, n_sink
         c.n_sessions, c.n_kv_heads, rows, c.head_dim = k.shape
@@ -490,11 +489,13 @@ class TokenCache:
         self._h = self.handle.value
 
     def _rows(self, name, t, width, n):
-        """Checks a matrix of the call ([n, width] or [n, heads, head_dim], rows any stride apart); returns (address, stride)."""
-        if t.dtype != self.dtype or t.device != self.device or t.shape[0] != n or t.numel() != n * width or t.stride(-1) != 1 \
-                or not (t.dim() == 2 or (t.dim() == 3 and t.shape[2] == self.head_dim and t.stride(1) == self.head_dim)):
-            raise ValueError(f"{name}: {n} rows of {width} {self.dtype} values on {self.device} are wanted, not {tuple(t.shape)} {t.dtype} on {t.device}")
-        return t.data_ptr(), t.stride(0) if n > 1 else max(t.stride(0), width)
+        """Checks a matrix of the call ([n, width] or [n, heads, head_dim], rows any stride apart); returns (address, stride).  (The checks are a good
+        part of a single token's call: few and cheap ones.)"""
+        st, d = t.stride(), self.head_dim
+        if t.dtype is self.dtype and t.get_device() == self._index and (
+                (len(st) == 3 and t.shape == (n, width // d, d) and st[1] == d and st[2] == 1) or (len(st) == 2 and t.shape == (n, width) and st[1] == 1)):
+            return t.data_ptr(), st[0] if n > 1 else max(st[0], width)
+        raise ValueError(f"{name}: {n} rows of {width} {self.dtype} values on {self.device} are wanted, not {tuple(t.shape)} (strides {st}) {t.dtype} on {t.device}")
 
     def append(self, qkv, batch: TokenBatch, norm: QKNorm, q=None, stream=None):
         """dc_cache_append: qkv is [n_tokens, (heads + 2 kv_heads) * head_dim]; returns the normalised, rotated queries
@@ -503,11 +504,13 @@ class TokenCache:
         if q is None:
             import torch
             q = torch.empty(n, self.c_cfg.n_heads, self.head_dim, dtype=self.dtype, device=self.device)
-        if batch.device != self.device or norm.device != self.device or norm.head_dim != self.head_dim:
+        if batch.index != self._index or norm.index != self._index or norm.head_dim != self.head_dim:
             raise ValueError("the batch and the norm belong to another device or head_dim than the cache")
         x, xs = self._rows("qkv", qkv, self._qkv_width, n)
         y, ys = self._rows("q", q, self._q_width, n)
-        _check(self.lib.dc_cache_append(self._h, batch.address, norm.address, x, xs, y, ys, _token_stream(stream, self.device)), "dc_cache_append")
+        st = self._append(self._h, batch.address, norm.address, x, xs, y, ys, _raw_stream(self._index) if stream is None else _cuda_stream_handle(stream))
+        if st:
+            raise DCError(st, "dc_cache_append")
         return q
 
     def attend(self, q, batch: TokenBatch, out=None, scale: Optional[float] = None, stream=None):
@@ -516,12 +519,13 @@ class TokenCache:
         if out is None:
             import torch
             out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        if batch.device != self.device:
+        if batch.index != self._index:
             raise ValueError("the batch belongs to another device than the cache")
         x, xs = self._rows("q", q, self._q_width, n)
         y, ys = self._rows("out", out, self._q_width, n)
-        _check(self.lib.dc_cache_attend(self._h, batch.address, x, xs, self.scale if scale is None else scale, y, ys, _token_stream(stream, self.device)),
-               "dc_cache_attend")
+        st = self._attend(self._h, batch.address, x, xs, self.scale if scale is None else scale, y, ys, _raw_stream(self._index) if stream is None else _cuda_stream_handle(stream))
+        if st:
+            raise DCError(st, "dc_cache_attend")
         return out
 
     def check(self):
@@ -549,15 +553,19 @@ def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError(f"logits: CUDA rows [rows, vocab] are wanted, not {tuple(logits.shape)}")
     n, vocab = logits.shape
-    f32, i32, dev = torch.float32, torch.int32, logits.device
+    f32, i32, at, stride = torch.float32, torch.int32, logits.get_device(), logits.stride(0)
     if tokens is None:
-        tokens = torch.empty(n, dtype=i32, device=dev)
-    r = dc_sample_rules(C.sizeof(dc_sample_rules), _vector("temperature", temperature, f32, n, dev), _vector("top_k", top_k, i32, n, dev),
-                        _vector("top_p", top_p, f32, n, dev), _vector("min_p", min_p, f32, n, dev))
-    _check(load_library().dc_sample_tokens(logits.data_ptr(), _dtype_code(logits), n, vocab, logits.stride(0) if n > 1 else max(logits.stride(0), vocab), C.byref(r),
-                                           _vector("u", u, f32, n, dev), _vector("tokens", tokens, i32, n, dev), _vector("probs", probs, f32, n, dev),
-                                           _token_stream(stream, dev)), "dc_sample_tokens")
+        tokens = torch.empty(n, dtype=i32, device=logits.device)
+    r = dc_sample_rules(_RULES_SIZE, _vector("temperature", temperature, f32, n, at), _vector("top_k", top_k, i32, n, at), _vector("top_p", top_p, f32, n, at),
+                        _vector("min_p", min_p, f32, n, at))
+    st = load_library().dc_sample_tokens(logits.data_ptr(), _dtype_code(logits), n, vocab, stride if n > 1 else max(stride, vocab), C.byref(r), _vector("u", u, f32, n, at),
+                                         _vector("tokens", tokens, i32, n, at), _vector("probs", probs, f32, n, at), _raw_stream(at) if stream is None else _cuda_stream_handle(stream))
+    if st:
+        raise DCError(st, "dc_sample_tokens")
     return tokens
+
+
+_RULES_SIZE = C.sizeof(dc_sample_rules)
 
 
 def _on(device):
@@ -565,9 +573,9 @@ def _on(device):
     return torch.cuda.device(device)
 
 
-def _token_stream(stream, device):
-    """The given stream, or the current one of the tensors' device (which need not be the current device)."""
-    if stream is not None:
-        return stream if isinstance(stream, int) else stream.cuda_stream
+def _raw_stream(index: int) -> int:
+    """The current stream of a device (which need not be the current device): the tensors' own."""
+    global _raw_stream
     import torch
-    return torch.cuda.current_stream(device).cuda_stream
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw_stream(index)
