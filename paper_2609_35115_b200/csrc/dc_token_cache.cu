@@ -226,34 +226,42 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   return v;
 }
 
-constexpr int STEP_WARPS = 4;
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
 constexpr int STEP_STAGES = 3;
 constexpr int STEP_HALF = 4096;                         // bytes of K, and of V, in a unit
 constexpr int STEP_UNIT = 2 * STEP_HALF;
-constexpr int STEP_SMEM = STEP_WARPS * STEP_STAGES * STEP_UNIT;
-constexpr int STEP_ROWS = 16;                           // query heads that one CTA serves (the rows of its products)
+constexpr int STEP_HEADS = 16;                          // query heads that one CTA serves at most
+constexpr int step_smem(int warps) { return warps * STEP_STAGES * STEP_UNIT; }
 
 // Bound by the reads of K and V, so the work is laid out for loads: a unit is 4 KB of K rows and the same V rows (16 rows of 128
 // values, 32 of 64), every warp streams units of its own through three stages of asynchronous 16-byte copies and keeps its own
-// running maximum, sum and output in registers; no warp waits for another before the end.  The query heads that share a K/V head are
-// the 16 rows of the matrix products (m16n8k16), so a row of K and V is read once for all of them.  The units of a
+// running maximum, sum and output in registers; no warp waits for another before the end.  The products (m16n8k16) have the rows of K, or the
+// columns of V, as their 16 rows and the query heads that share a K/V head as their 8 columns (NH = 2: twice 8): a row is read once for
+// all of them, and a group of up to 8 heads takes 8 + 16 products a unit.  (With the heads as the 16 rows it took 48, and
+// those, at about 35 cycles each, bounded the kernel: 36 us against 18 for one session of 32,768 rows.)  The units of a
 // (sequence, head) are dealt out over the warps of a cluster of CTAs, which joins the partial results through distributed shared
 // memory: no workspace, no second launch.  The numerators enter the second product as two halves (their rounding to 16 bits and what
-// that leaves): the products are a tenth of the time that the reads take.
-template <typename T, int D>
-__global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const AttendArgs a) {
+// that leaves), so that the result is rounded once.
+template <typename T, int D, int NH, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) attend_step_kernel(const AttendArgs a) {
   constexpr int UN = STEP_HALF / (2 * D);    // rows of a unit
   constexpr int CPR = D / 8;                 // 16-byte chunks of a row
-  constexpr int NT = UN / 8, KS = D / 16, DT = D / 8;
+  constexpr int MT = UN / 16, KS = D / 16, DT = D / 16;
+  constexpr int PD = D + 8;                  // floats between two heads of a partial output
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ float wm[STEP_WARPS][STEP_ROWS], wl[STEP_WARPS][STEP_ROWS];
-  __shared__ float cm[STEP_ROWS], cl[STEP_ROWS];
+  __shared__ float wm[WARPS][STEP_HEADS], wl[WARPS][STEP_HEADS];
+  __shared__ float cm[STEP_HEADS], cl[STEP_HEADS];
   ptx::pdl_wait();
   ptx::pdl_launch();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int rank = blockIdx.x;   // in the cluster: gridDim.x == splits
-  const int groups = (a.group + STEP_ROWS - 1) / STEP_ROWS;
-  const int kvh = blockIdx.y / groups, h0 = (blockIdx.y % groups) * STEP_ROWS, nh = min(STEP_ROWS, a.group - h0);
+  const int groups = (a.group + 8 * NH - 1) / (8 * NH);
+  const int kvh = blockIdx.y / groups, h0 = (blockIdx.y % groups) * (8 * NH), nh = min(8 * NH, a.group - h0);
   const TokenSeq s = load_seq(a.b, a.d, blockIdx.z);
   if (s.count != 1) return;      // (the whole cluster)
   const int pos = s.start, rows = a.d.n_sink + a.d.ring;
@@ -266,7 +274,7 @@ __global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const Atte
 
   uint8_t* ring = smem + warp * STEP_STAGES * STEP_UNIT;
   const uint32_t ring_s = ptx::smem_u32(ring);
-  const int step = a.splits * STEP_WARPS;
+  const int step = a.splits * WARPS;
   auto unit_rows = [&](int u, int& row0) {
     row0 = u < u_first ? u * UN : lo2 + (u - u_first) * UN;
     return u < u_first ? n_first - row0 : n_second - (u - u_first) * UN;   // (may exceed UN)
@@ -288,28 +296,32 @@ __global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const Atte
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  int u = rank * STEP_WARPS + warp;
+  int u = rank * WARPS + warp;
 #pragma unroll
   for (int i = 0; i < STEP_STAGES - 1; ++i) fetch(u + i * step, i);
 
-  // the queries as the first operand: rows g and g + 8
-  uint32_t qf[KS][4];
+  // the queries as the second operand: head g of each eight
+  uint32_t qf[NH][KS][2];
   {
     const T* q = static_cast<const T*>(a.q) + (long long)s.first * a.q_stride + (long long)(kvh * a.group + h0) * D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int h = 0; h < NH; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = g + (i & 1) * 8, c = ks * 16 + t * 2 + (i >> 1) * 8;
-        qf[ks][i] = r < nh ? *reinterpret_cast<const uint32_t*>(q + r * D + c) : 0u;
-      }
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) qf[h][ks][i] = h * 8 + g < nh ? *reinterpret_cast<const uint32_t*>(q + (h * 8 + g) * D + ks * 16 + t * 2 + i * 8) : 0u;
   }
-  float o[DT][4];
+  // of heads 2 t and 2 t + 1 of each eight; output columns g and g + 8 of each sixteen
+  float o[NH][DT][4], m[NH][2], l[NH][2];
 #pragma unroll
-  for (int j = 0; j < DT; ++j)
+  for (int h = 0; h < NH; ++h) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int j = 0; j < DT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[h][j][i] = 0.f;
+    m[h][0] = m[h][1] = -INFINITY;
+    l[h][0] = l[h][1] = 0.f;
+  }
 
   int stage = 0;
   for (; u < units; u += step) {
@@ -320,76 +332,93 @@ __global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const Atte
     stage = stage + 1 == STEP_STAGES ? 0 : stage + 1;
     int row0;
     const int n = unit_rows(u, row0);
-    float sc[NT][4];
+    float sc[NH][MT][4];     // keys g (0, 1) and g + 8 (2, 3) of each sixteen, heads 2 t and 2 t + 1
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sc[j][i] = 0.f;
+      for (int h = 0; h < NH; ++h)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+        for (int i = 0; i < 4; ++i) sc[h][mt][i] = 0.f;
 #pragma unroll
-      for (int j = 0; j < NT; j += 2) {
+      for (int ks = 0; ks < KS; ++ks) {
         uint32_t kf[4];
-        const int r = (j + (lane >> 4)) * 8 + (lane & 7), c = 2 * ks + ((lane >> 3) & 1);
+        const int r = mt * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), c = 2 * ks + (lane >> 4);
         ldsm4(ks_ + r * (2 * D) + ((c ^ (r & 7)) << 4), kf);
-        mma16816<T>(sc[j], qf[ks], kf[0], kf[1]);
-        mma16816<T>(sc[j + 1], qf[ks], kf[2], kf[3]);
+#pragma unroll
+        for (int h = 0; h < NH; ++h) mma16816<T>(sc[h][mt], kf, qf[h][ks][0], qf[h][ks][1]);
       }
-    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = j * 8 + t * 2 + (i & 1) < n ? sc[j][i] * a.scale_log2e : -INFINITY;
-        sc[j][i] = x;
-        top[i >> 1] = fmaxf(top[i >> 1], x);
-      }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
     }
-    if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
+    float top[NH][2];
+    bool move = false;
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float mn = fmaxf(m[i], top[i]);
-        const float f = mn > m[i] ? ex2(m[i] - mn) : 1.f;     // (m = -inf: 0)
-        m[i] = mn;
-        l[i] *= f;
+        float x = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < DT; ++j) {
-          o[j][2 * i] *= f;
-          o[j][2 * i + 1] *= f;
-        }
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float& y = sc[h][mt][2 * k + i];
+            y = mt * 16 + 8 * k + g < n ? y * a.scale_log2e : -INFINITY;
+            x = fmaxf(x, y);
+          }
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+        top[h][i] = x;
+        move |= x > m[h][i] + 8.f;      // (m = -infinity: at the first row)
       }
     }
-    const float base[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+    // the running maximum moves when it is passed by 2^8: numerators stay within the types' range, the output is rescaled seldom
+    if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int h = 0; h < NH; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sc[j][i] = ex2(sc[j][i] - base[i >> 1]);
-        l[i >> 1] += sc[j][i];
-      }
+        for (int i = 0; i < 2; ++i) {
+          const float mn = fmaxf(m[h][i], top[h][i]), f = mn > m[h][i] ? ex2(m[h][i] - mn) : 1.f;
+          m[h][i] = mn;
+          l[h][i] *= f;
 #pragma unroll
-    for (int kk = 0; kk < NT / 2; ++kk) {
-      uint32_t hi[4], lo[4];
+          for (int j = 0; j < DT; ++j) {
+            o[h][j][i] *= f;
+            o[h][j][2 + i] *= f;
+          }
+        }
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = sc[2 * kk + (i >> 1)][(i & 1) * 2], y = sc[2 * kk + (i >> 1)][(i & 1) * 2 + 1];
-        hi[i] = Num<T>::pack(x, y);
-        const float2 r = Num<T>::unpack(hi[i]);
-        lo[i] = Num<T>::pack(x - r.x, y - r.y);
-      }
+    for (int h = 0; h < NH; ++h) {
+      const float base[2] = {m[h][0] == -INFINITY ? 0.f : m[h][0], m[h][1] == -INFINITY ? 0.f : m[h][1]};
 #pragma unroll
-      for (int j = 0; j < DT; j += 2) {
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[h][mt][i] = ex2(sc[h][mt][i] - base[i & 1]);
+          l[h][i & 1] += sc[h][mt][i];
+        }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      uint32_t hi[NH][2], lo[NH][2];      // keys 0 .. 7 and 8 .. 15 of the sixteen, as the second operand
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float x = sc[h][mt][2 * k], y = sc[h][mt][2 * k + 1];
+          const uint32_t p = Num<T>::pack(x, y);
+          const float2 r = Num<T>::unpack(p);
+          hi[h][k] = transpose8x8(p);
+          lo[h][k] = transpose8x8(Num<T>::pack(x - r.x, y - r.y));
+        }
+#pragma unroll
+      for (int j = 0; j < DT; ++j) {
         uint32_t vf[4];
-        const int r = kk * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), c = j + (lane >> 4);
+        const int r = mt * 16 + (lane >> 4) * 8 + (lane & 7), c = 2 * j + ((lane >> 3) & 1);
         ldsm4t(vs_ + r * (2 * D) + ((c ^ (r & 7)) << 4), vf);
-        mma16816<T>(o[j], hi, vf[0], vf[1]);
-        mma16816<T>(o[j + 1], hi, vf[2], vf[3]);
-        mma16816<T>(o[j], lo, vf[0], vf[1]);
-        mma16816<T>(o[j + 1], lo, vf[2], vf[3]);
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+          mma16816<T>(o[h][j], vf, hi[h][0], hi[h][1]);
+          mma16816<T>(o[h][j], vf, lo[h][0], lo[h][1]);
+        }
       }
     }
   }
@@ -397,36 +426,41 @@ __global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const Atte
   __syncwarp();
 
   // ---- join: the warps of the CTA, then the CTAs of the cluster -----------------------------------------------------------
+  float* part = reinterpret_cast<float*>(ring);     // [heads][PD] of this warp (at most 9 KB of its 24)
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    if (t == 0) {
-      wm[warp][g + 8 * i] = m[i];
-      wl[warp][g + 8 * i] = l[i];
+  for (int h = 0; h < NH; ++h)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) l[h][i] += __shfl_xor_sync(0xffffffffu, l[h][i], d);
+      const int head = h * 8 + 2 * t + i;
+      if (g == 0) {
+        wm[warp][head] = m[h][i];
+        wl[warp][head] = l[h][i];
+      }
+      if (head < nh) {
+#pragma unroll
+        for (int j = 0; j < DT; ++j) {
+          part[head * PD + j * 16 + g] = o[h][j][i];
+          part[head * PD + j * 16 + 8 + g] = o[h][j][2 + i];
+        }
+      }
     }
-  }
-  float* part = reinterpret_cast<float*>(ring);     // [16][D] of this warp (8 KB of its 24)
-#pragma unroll
-  for (int j = 0; j < DT; ++j)
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (g + 8 * i < nh) *reinterpret_cast<float2*>(part + (g + 8 * i) * D + j * 8 + t * 2) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
   __syncthreads();
   constexpr int WSTRIDE = STEP_STAGES * STEP_UNIT / 4;   // floats between two warps' parts
   float* all = reinterpret_cast<float*>(smem);
   T* out = static_cast<T*>(a.out) + (long long)s.first * a.out_stride + (long long)(kvh * a.group + h0) * D;
-  for (int e = threadIdx.x * 2; e < nh * D; e += STEP_WARPS * 64) {
-    const int r = e / D;
+  for (int e = threadIdx.x * 2; e < nh * D; e += WARPS * 64) {
+    const int r = e / D, at = r * PD + e % D;
     float M = wm[0][r];
 #pragma unroll
-    for (int w = 1; w < STEP_WARPS; ++w) M = fmaxf(M, wm[w][r]);
+    for (int w = 1; w < WARPS; ++w) M = fmaxf(M, wm[w][r]);
     const float base = M == -INFINITY ? 0.f : M;
     float x = 0.f, y = 0.f, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < STEP_WARPS; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
       const float f = ex2(wm[w][r] - base);
-      const float2 v = *reinterpret_cast<const float2*>(all + w * WSTRIDE + e);
+      const float2 v = *reinterpret_cast<const float2*>(all + w * WSTRIDE + at);
       x = fmaf(f, v.x, x);
       y = fmaf(f, v.y, y);
       L = fmaf(f, wl[w][r], L);
@@ -435,7 +469,7 @@ __global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const Atte
       const float inv = 1.0f / L;
       *reinterpret_cast<uint32_t*>(out + e) = Num<T>::pack(x * inv, y * inv);
     } else {
-      *reinterpret_cast<float2*>(all + e) = make_float2(x, y);     // (each element is read and written by one thread)
+      *reinterpret_cast<float2*>(all + at) = make_float2(x, y);     // (each element is read and written by one thread)
       if (e % D == 0) {
         cm[r] = M;
         cl[r] = L;
@@ -446,18 +480,19 @@ __global__ void __launch_bounds__(STEP_WARPS * 32) attend_step_kernel(const Atte
   ptx::cluster_arrive();
   ptx::cluster_wait();
   const uint32_t all_s = ptx::smem_u32(all), cm_s = ptx::smem_u32(cm), cl_s = ptx::smem_u32(cl);
-  for (int e = (rank * STEP_WARPS * 32 + (int)threadIdx.x) * 2; e < nh * D; e += a.splits * STEP_WARPS * 64) {
-    const int r = e / D;
+  for (int e = (rank * WARPS * 32 + (int)threadIdx.x) * 2; e < nh * D; e += a.splits * WARPS * 64) {
+    const int r = e / D, at = r * PD + e % D;
     float M = -INFINITY;
+#pragma unroll 4
     for (int c = 0; c < a.splits; ++c) M = fmaxf(M, ld_cluster(ptx::map_to_cta(cm_s + r * 4, c)));
     const float base = M == -INFINITY ? 0.f : M;
     float x = 0.f, y = 0.f, L = 0.f;
 #pragma unroll 4
     for (int c = 0; c < a.splits; ++c) {
       const float f = ex2(ld_cluster(ptx::map_to_cta(cm_s + r * 4, c)) - base);
-      const uint32_t at = ptx::map_to_cta(all_s + e * 4, c);
-      x = fmaf(f, ld_cluster(at), x);
-      y = fmaf(f, ld_cluster(at + 4), y);
+      const uint32_t from = ptx::map_to_cta(all_s + at * 4, c);
+      x = fmaf(f, ld_cluster(from), x);
+      y = fmaf(f, ld_cluster(from + 4), y);
       L = fmaf(f, ld_cluster(ptx::map_to_cta(cl_s + r * 4, c)), L);
     }
     const float inv = 1.0f / L;
@@ -556,10 +591,15 @@ AppendFn append_fn(int dtype, int D, bool inter) {
   return D == 128 ? (inter ? append_kernel<__half, 128, true> : append_kernel<__half, 128, false>)
                   : (inter ? append_kernel<__half, 64, true> : append_kernel<__half, 64, false>);
 }
-StepFn step_fn(int dtype, int D) {
+template <typename T, int D>
+StepFn step_of(bool two, bool wide) {
   using namespace dc;
-  if (dtype == DC_BF16) return D == 128 ? attend_step_kernel<bf16, 128> : attend_step_kernel<bf16, 64>;
-  return D == 128 ? attend_step_kernel<__half, 128> : attend_step_kernel<__half, 64>;
+  return two ? (wide ? attend_step_kernel<T, D, 2, 8> : attend_step_kernel<T, D, 2, 4>) : (wide ? attend_step_kernel<T, D, 1, 8> : attend_step_kernel<T, D, 1, 4>);
+}
+// two: groups of more than 8 query heads; wide: CTAs of 8 warps
+StepFn step_fn(int dtype, int D, bool two, bool wide) {
+  if (dtype == DC_BF16) return D == 128 ? step_of<dc::bf16, 128>(two, wide) : step_of<dc::bf16, 64>(two, wide);
+  return D == 128 ? step_of<__half, 128>(two, wide) : step_of<__half, 64>(two, wide);
 }
 
 using ChunkFn = void (*)(const dc::ChunkArgs);
@@ -616,8 +656,11 @@ extern "C" dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void
     delete c;
     DC_REFUSE(DC_ERR_CUDA, "dc_cache_open: this library is built for sm_100a only");
   }
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim), cudaFuncAttributeMaxDynamicSharedMemorySize, dc::STEP_SMEM);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  const bool two = cfg->n_heads / cfg->n_kv_heads > 8;
+  for (int wide = 0; wide < 2; ++wide) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim, two, wide), cudaFuncAttributeMaxDynamicSharedMemorySize, dc::step_smem(wide ? 8 : 4));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim, two, wide), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  }
   if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)chunk_smem_bytes(c->head_dim));
   if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess && !(cache_map(&c->kmap, c, k_dev) && cache_map(&c->vmap, c, v_dev))) {
@@ -698,10 +741,14 @@ extern "C" dc_status dc_cache_attend(dc_cache* c, const dc_token_batch* b, const
     return launched(dc::launch(chunk_fn(c->dtype, D), dim3(ca.tiles * ca.a.splits, c->d.n_kv_heads, b->n_seqs), dc::CH_THREADS, chunk_smem_bytes(D), ca.a.splits,
                                (cudaStream_t)cuda_stream, &ca), who);
   }
-  const int groups = (a.group + dc::STEP_ROWS - 1) / dc::STEP_ROWS;
-  // Splits: as many CTAs as two waves' worth of SMs hold, while every warp has a unit of its own.
+  const bool two = a.group > 8;
+  const int per = two ? 16 : 8, groups = (a.group + per - 1) / per;
   const long long units = seen * D * 2 / dc::STEP_HALF + 1, pairs = (long long)b->n_seqs * c->d.n_kv_heads * groups;
-  while (a.splits < 16 && pairs * a.splits * 2 <= 2ll * c->n_sm && (long long)a.splits * 2 * dc::STEP_WARPS <= units) a.splits *= 2;
-  return launched(dc::launch(step_fn(c->dtype, D), dim3(a.splits, c->d.n_kv_heads * groups, b->n_seqs), dc::STEP_WARPS * 32, dc::STEP_SMEM, a.splits,
+  // Splits: while every warp has a unit of its own, and either the CTAs are resident (two per SM) or, of many long rows, up to four
+  // for the balance of the last wave (48 sessions x 8 heads of 4,100 rows: 126 us unsplit, 115 us in two or four, 148 us in eight).
+  while (a.splits < 16 && a.splits * 2 * 4 <= units && (pairs * a.splits * 2 <= 2ll * c->n_sm || (a.splits < 4 && units >= 64 * a.splits))) a.splits *= 2;
+  // CTAs of 8 warps, one per SM, where there are fewer CTAs than SMs and rows enough: the copies in flight on an SM are what bounds it then.
+  const bool wide = pairs * a.splits <= c->n_sm && (long long)a.splits * 8 * 2 <= units;
+  return launched(dc::launch(step_fn(c->dtype, D, two, wide), dim3(a.splits, c->d.n_kv_heads * groups, b->n_seqs), wide ? 256 : 128, dc::step_smem(wide ? 8 : 4), a.splits,
                              (cudaStream_t)cuda_stream, &a), who);
 }
