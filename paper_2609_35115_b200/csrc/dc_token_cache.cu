@@ -205,13 +205,13 @@ template <typename T>
 __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1);
 template <>
 __device__ __forceinline__ void mma16816<bf16>(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <>
 __device__ __forceinline__ void mma16816<__half>(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -228,7 +228,7 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 
@@ -332,22 +332,40 @@ __global__ void __launch_bounds__(WARPS * 32) attend_step_kernel(const AttendArg
     stage = stage + 1 == STEP_STAGES ? 0 : stage + 1;
     int row0;
     const int n = unit_rows(u, row0);
-    float sc[NH][MT][4];     // keys g (0, 1) and g + 8 (2, 3) of each sixteen, heads 2 t and 2 t + 1
+    // all of the unit's rows of K go to registers first, the products of a sixteen run as two chains
+    uint32_t kf[MT][KS][4];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sc[h][mt][i] = 0.f;
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        uint32_t kf[4];
         const int r = mt * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), c = 2 * ks + (lane >> 4);
-        ldsm4(ks_ + r * (2 * D) + ((c ^ (r & 7)) << 4), kf);
-#pragma unroll
-        for (int h = 0; h < NH; ++h) mma16816<T>(sc[h][mt], kf, qf[h][ks][0], qf[h][ks][1]);
+        ldsm4(ks_ + r * (2 * D) + ((c ^ (r & 7)) << 4), kf[mt][ks]);
       }
-    }
+    float sc[NH][MT][4];     // keys g (0, 1) and g + 8 (2, 3) of each sixteen, heads 2 t and 2 t + 1
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        float odd[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[h][mt][i] = odd[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks += 2) {
+          mma16816<T>(sc[h][mt], kf[mt][ks], qf[h][ks][0], qf[h][ks][1]);
+          mma16816<T>(odd, kf[mt][ks + 1], qf[h][ks + 1][0], qf[h][ks + 1][1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[h][mt][i] += odd[i];
+      }
+    // ... and so do the columns of V, under the softmax
+    uint32_t vf[MT][DT][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int j = 0; j < DT; ++j) {
+        const int r = mt * 16 + (lane >> 4) * 8 + (lane & 7), c = 2 * j + ((lane >> 3) & 1);
+        ldsm4t(vs_ + r * (2 * D) + ((c ^ (r & 7)) << 4), vf[mt][j]);
+      }
     float top[NH][2];
     bool move = false;
 #pragma unroll
@@ -410,15 +428,11 @@ __global__ void __launch_bounds__(WARPS * 32) attend_step_kernel(const AttendArg
           lo[h][k] = transpose8x8(Num<T>::pack(x - r.x, y - r.y));
         }
 #pragma unroll
-      for (int j = 0; j < DT; ++j) {
-        uint32_t vf[4];
-        const int r = mt * 16 + (lane >> 4) * 8 + (lane & 7), c = 2 * j + ((lane >> 3) & 1);
-        ldsm4t(vs_ + r * (2 * D) + ((c ^ (r & 7)) << 4), vf);
+      for (int h = 0; h < NH; ++h) {
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          mma16816<T>(o[h][j], vf, hi[h][0], hi[h][1]);
-          mma16816<T>(o[h][j], vf, lo[h][0], lo[h][1]);
-        }
+        for (int j = 0; j < DT; ++j) mma16816<T>(o[h][j], vf[mt][j], hi[h][0], hi[h][1]);
+#pragma unroll
+        for (int j = 0; j < DT; ++j) mma16816<T>(o[h][j], vf[mt][j], lo[h][0], lo[h][1]);
       }
     }
   }
