@@ -39,23 +39,28 @@ template <> struct Num<__half> {
   }
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* x, bf16) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = Num<bf16>::unpack(w[i]);
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
+// 16 bytes global -> shared, asynchronously; off: zeros, and the source is not read.
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void unpack8(const uint4& v, float* x, __half) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = Num<__half>::unpack(w[i]);
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(d)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return d;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -70,21 +75,38 @@ struct AppendArgs {
   const float *q_gain, *k_gain, *inv_freq;
   int         rot;
   float       eps;
+  int         share;     // warps that a token's row is dealt out over
 };
 
-constexpr int APPEND_THREADS = 256;
-constexpr int APPEND_MAX_CHUNKS = 4;   // 16-byte pieces of a row that a thread has in flight
+constexpr int APPEND_WARPS = 8;
+constexpr int APPEND_DEPTH = 8;    // 16-byte pieces that a lane has in flight
 
-// One CTA per token.  A head is D / 8 neighbouring lanes of 16 bytes each, so the sum of squares and the partner of a
-// rotated pair come from shuffles and every value is read once and written once.  The angle is position * inv_freq in
-// 64 bits, in turns, whose fraction is exact enough in 32 for sincospi: rot / 2 of them per token, shared by all heads.
+// Bound by the reads and writes of the rows.  Warps work alone, `share` of them on a token: all of a CTA's for single tokens, where the
+// latency of one row counts, one for prompts, where the look-up of the token's sequence and its angles are paid once for the whole row.
+// A head is D / 8 neighbouring lanes of 16 bytes each, so the sum of squares and the partner of a
+// rotated pair come from shuffles, every value is read once and written once, and a lane's gains and angles are the same for
+// all heads; two values go through each operation.  The angle is position * inv_freq in 64 bits, in turns, whose fraction is exact enough in 32 for sincospi.
 template <typename T, int D, bool INTER>
-__global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(APPEND_WARPS * 32, 3) append_kernel(const AppendArgs a) {
   constexpr int LPH = D / 8;
-  __shared__ float2 turn[D / 2];
+  __shared__ uint4 rings[APPEND_WARPS][APPEND_DEPTH * 32];
+  __shared__ __align__(16) float2 turns[APPEND_WARPS][D / 2];
   ptx::pdl_wait();
   ptx::pdl_launch();
-  const int token = blockIdx.x, lane = threadIdx.x & 31, half = a.rot / 2;
+  const int lane = threadIdx.x & 31, id = blockIdx.x * APPEND_WARPS + (threadIdx.x >> 5), half = a.rot / 2, l = lane % LPH;
+  const int token = id / a.share, part = id % a.share;
+  if (token >= a.b.n_tokens) return;
+  const int q_end = a.d.n_heads * LPH, k_end = q_end + a.d.n_kv_heads * LPH, chunks = k_end + a.d.n_kv_heads * LPH, step = 32 * a.share;
+  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.qkv) + (long long)token * a.qkv_stride);
+  // the row's pieces come through a ring of shared memory, each lane's its own: nobody waits for another's (a row behind the last sequence
+  // is read for nothing)
+  uint4* ring = rings[threadIdx.x >> 5] + lane;
+  auto fetch = [&](int c, int slot) {
+    if (c < chunks) cp16(ptx::smem_u32(ring + slot * 32), src + c, true);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int u = 0; u < APPEND_DEPTH; ++u) fetch(part * 32 + u * step + lane, u);
   // the token's sequence: the boundaries at or below it, counted 32 at a time
   int seq = token;
   if (a.b.cu_tokens) {
@@ -95,86 +117,110 @@ __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(const AppendArgs
       seq += __popc(le);
       if (le != 0xffffffffu) break;
     }
-    if (seq < 0 || seq >= a.b.n_seqs) return;   // a row behind the last sequence
   }
-  const TokenSeq s = load_seq(a.b, a.d, seq);
-  if (token - s.first >= s.count || token < s.first) return;
+  TokenSeq s{};
+  if (seq >= 0 && seq < a.b.n_seqs) s = load_seq(a.b, a.d, seq);
+  if (token - s.first >= s.count || token < s.first) {      // no sequence's row, or one that does not fit
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    return;
+  }
   const int pos = s.start + (token - s.first);
-  if ((int)threadIdx.x < half) {
-    const double t = (double)pos * (double)a.inv_freq[threadIdx.x] * 0.15915494309189533577;
+  float2* turn = turns[threadIdx.x >> 5];
+  for (int j = lane; j < half; j += 32) {
+    const double t = (double)pos * (double)a.inv_freq[j] * 0.15915494309189533577;
     float sn, cs;
     sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
-    turn[threadIdx.x] = make_float2(cs, sn);
+    turn[j] = make_float2(cs, sn);
   }
-  const int H = a.d.n_heads, Hkv = a.d.n_kv_heads, chunks = (H + 2 * Hkv) * LPH;
-  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.qkv) + (long long)token * a.qkv_stride);
-  const long long row = cache_row(a.d, pos), rows = a.d.n_sink + a.d.ring;
-  const int l = threadIdx.x % LPH;
-  bool synced = false;
-  for (int c0 = 0; c0 < chunks; c0 += APPEND_MAX_CHUNKS * blockDim.x) {
-    uint4 in[APPEND_MAX_CHUNKS];
+  __syncwarp();
+  // This lane's part of gain and rotation, for q and for k: y = (x c + other s) / rms, where `other` is the other value of the pair (its
+  // neighbour, or the same place of the lane half a rotated head away), c the value's gain times the cosine, s the other's gain times the sine.
+  const int hl = half / 8;
+  const bool lower = l < hl, turned = INTER ? 8 * l < a.rot : l < 2 * hl;
+  const int partner = INTER || !turned ? lane : lane + (lower ? hl : -hl), lp = partner % LPH;
+  float2 mc[2][4], ms[2][4];
+  {
+    float cs[8], sn[8];      // (16 bytes a load: there are many of these values for a row of few heads)
+    const float4* t4 = reinterpret_cast<const float4*>(turn + (turned ? (INTER ? 4 * l : 8 * (lower ? l : l - hl)) : 0));
 #pragma unroll
-    for (int u = 0; u < APPEND_MAX_CHUNKS; ++u) {
-      const int c = c0 + u * (int)blockDim.x + (int)threadIdx.x;
-      in[u] = c < chunks ? src[c] : make_uint4(0, 0, 0, 0);
-    }
-    if (!synced) __syncthreads();
-    synced = true;
-#pragma unroll
-    for (int u = 0; u < APPEND_MAX_CHUNKS; ++u) {
-      const int c = c0 + u * (int)blockDim.x + (int)threadIdx.x, head = c / LPH;
-      if (c - lane >= chunks) break;   // (the whole warp)
-      uint4 out = in[u];
-      // a warp's pieces may belong to q or k and to v at once (head_dim 64: four heads of a warp): all lanes go through the shuffles
-      float x[8], ss = 0.f;
-      unpack8(in[u], x, T());
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-#pragma unroll
-      for (int m = LPH / 2; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-      const float r = rsqrtf(ss * (1.0f / D) + a.eps);
-      const float4* g = reinterpret_cast<const float4*>(head < H ? a.q_gain : a.k_gain) + 2 * l;
-      const float4 g0 = __ldg(g), g1 = __ldg(g + 1);
-      const float gain[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = x[i] * r * gain[i];
+    for (int i = 0; i < (INTER ? 2 : 4); ++i) {
+      const float4 t = turned ? t4[i] : make_float4(1.f, 0.f, 1.f, 0.f);
       if (INTER) {
-        if (8 * l < a.rot) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 t = turn[4 * l + i];
-            const float p = x[2 * i], q = x[2 * i + 1];
-            x[2 * i] = p * t.x - q * t.y;
-            x[2 * i + 1] = q * t.x + p * t.y;
-          }
-        }
+        cs[4 * i] = cs[4 * i + 1] = t.x;
+        cs[4 * i + 2] = cs[4 * i + 3] = t.z;
+        sn[4 * i] = -t.y;
+        sn[4 * i + 1] = t.y;
+        sn[4 * i + 2] = -t.w;
+        sn[4 * i + 3] = t.w;
       } else {
-        const int hl = half / 8;   // lanes of half a rotated head
-        const bool lower = l < hl;
-        const int partner = lane + (lower ? hl : l < 2 * hl ? -hl : 0);
-        float o[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = __shfl_sync(0xffffffffu, x[i], partner);
-        if (l < 2 * hl) {
-          const float2* t = turn + 8 * (lower ? l : l - hl);
-          const float sign = lower ? -1.f : 1.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = x[i] * t[i].x + sign * (o[i] * t[i].y);
-        }
+        cs[2 * i] = t.x;
+        cs[2 * i + 1] = t.z;
+        sn[2 * i] = lower ? -t.y : t.y;
+        sn[2 * i + 1] = lower ? -t.w : t.w;
       }
-      if (head < H + Hkv)
-        out = make_uint4(Num<T>::pack(x[0], x[1]), Num<T>::pack(x[2], x[3]), Num<T>::pack(x[4], x[5]), Num<T>::pack(x[6], x[7]));
-      if (c >= chunks) continue;
-      T* dst;
-      if (head < H) {
-        dst = static_cast<T*>(a.q) + (long long)token * a.q_stride + (long long)head * D;
-      } else {
-        const int h = head < H + Hkv ? head - H : head - H - Hkv;
-        dst = static_cast<T*>(head < H + Hkv ? a.k : a.v) + (((long long)s.session * Hkv + h) * rows + row) * D;
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const float4* g = reinterpret_cast<const float4*>(w ? a.k_gain : a.q_gain);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 mine = __ldg(g + 2 * l + i), far = INTER ? make_float4(mine.y, mine.x, mine.w, mine.z) : __ldg(g + 2 * lp + i);
+        mc[w][2 * i] = make_float2(mine.x * cs[4 * i], mine.y * cs[4 * i + 1]);
+        mc[w][2 * i + 1] = make_float2(mine.z * cs[4 * i + 2], mine.w * cs[4 * i + 3]);
+        ms[w][2 * i] = make_float2(far.x * sn[4 * i], far.y * sn[4 * i + 1]);
+        ms[w][2 * i + 1] = make_float2(far.z * sn[4 * i + 2], far.w * sn[4 * i + 3]);
       }
-      reinterpret_cast<uint4*>(dst)[l] = out;
     }
   }
+  auto normed = [&](const uint4& v, const float2 (&c)[4], const float2 (&n)[4]) {
+    const uint32_t own[4] = {v.x, v.y, v.z, v.w};
+    uint32_t far[4];
+    float2 x[4], sq = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = Num<T>::unpack(own[i]);
+      sq = fma2(x[i], x[i], sq);
+      if (!INTER) far[i] = __shfl_sync(0xffffffffu, own[i], partner);
+    }
+    float ss = sq.x + sq.y;
+#pragma unroll
+    for (int m = LPH / 2; m >= 1; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+    const float r = rsqrtf(ss * (1.0f / D) + a.eps);
+    uint32_t y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float2 z = mul2(x[i], c[i]);
+      if (turned) z = fma2(INTER ? make_float2(x[i].y, x[i].x) : Num<T>::unpack(far[i]), n[i], z);
+      z = mul2(z, make_float2(r, r));
+      y[i] = Num<T>::pack(z.x, z.y);
+    }
+    return make_uint4(y[0], y[1], y[2], y[3]);
+  };
+  uint4* q_row = reinterpret_cast<uint4*>(static_cast<T*>(a.q) + (long long)token * a.q_stride);
+  const long long plane = ((long long)a.d.n_sink + a.d.ring) * LPH, at = (long long)s.session * a.d.n_kv_heads * plane + (long long)cache_row(a.d, pos) * LPH + l;
+  uint4 *k_row = static_cast<uint4*>(a.k) + at, *v_row = static_cast<uint4*>(a.v) + at;
+  int slot = 0;
+  for (int first = part * 32; first < chunks; first += step) {
+    const int c = first + lane;
+    asm volatile("cp.async.wait_group %0;" ::"n"(APPEND_DEPTH - 1) : "memory");
+    const uint4 v = ring[slot * 32];
+    fetch(c + APPEND_DEPTH * step, slot);
+    slot = slot + 1 == APPEND_DEPTH ? 0 : slot + 1;
+    // heads of q only, of k only, of v only, or (where they meet inside of a warp's 32 pieces) of several kinds: each lane its own
+    if (first + 32 <= q_end) {
+      q_row[c] = normed(v, mc[0], ms[0]);
+    } else if (first >= q_end && first + 32 <= k_end) {
+      k_row[(c - q_end) / LPH * plane] = normed(v, mc[1], ms[1]);
+    } else if (first >= k_end) {
+      if (c < chunks) v_row[(c - k_end) / LPH * plane] = v;
+    } else {
+      const uint4 yq = normed(v, mc[0], ms[0]), yk = normed(v, mc[1], ms[1]);
+      if (c < q_end) q_row[c] = yq;
+      else if (c < k_end) k_row[(c - q_end) / LPH * plane] = yk;
+      else if (c < chunks) v_row[(c - k_end) / LPH * plane] = v;
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -192,9 +238,6 @@ struct AttendArgs {
   int*        err;
 };
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
@@ -726,10 +769,12 @@ extern "C" dc_status dc_cache_append(dc_cache* c, const dc_token_batch* b, const
   if (bad_rows(qkv_dev, qkv_stride, (long long)(c->d.n_heads + 2 * c->d.n_kv_heads) * D) || bad_rows(q_dev, q_stride, (long long)c->d.n_heads * D))
     DC_REFUSE(DC_ERR_ARG, "%s: qkv_dev and q_dev must be 16-byte aligned, their row strides multiples of 8 values and no shorter than a row", who);
   if (q_dev == qkv_dev && q_stride != qkv_stride) DC_REFUSE(DC_ERR_ARG, "%s: queries written in place keep the rows' stride", who);
-  const dc::AppendArgs a{c->d, kernel_batch(b), qkv_dev, qkv_stride, q_stride, q_dev, c->k, c->v, nm->q_gain_dev, nm->k_gain_dev, nm->inv_freq_dev, nm->rot_dim, nm->eps};
-  const int chunks = (c->d.n_heads + 2 * c->d.n_kv_heads) * D / 8;
-  const int threads = chunks >= dc::APPEND_THREADS ? dc::APPEND_THREADS : chunks <= 64 ? 64 : (chunks + 31) / 32 * 32;
-  return launched(dc::launch(append_fn(c->dtype, D, nm->interleaved != 0), dim3(b->n_tokens), threads, 0, 1, (cudaStream_t)cuda_stream, &a), who);
+  dc::AppendArgs a{c->d, kernel_batch(b), qkv_dev, qkv_stride, q_stride, q_dev, c->k, c->v, nm->q_gain_dev, nm->k_gain_dev, nm->inv_freq_dev, nm->rot_dim, nm->eps, dc::APPEND_WARPS};
+  // A token's row is dealt out over a whole CTA's warps while that gives an SM no more than 32 warps to run, and over fewer behind that.
+  while (a.share > 1 && (long long)b->n_tokens * a.share > 32ll * c->n_sm) a.share /= 2;
+  const long long warps = (long long)b->n_tokens * a.share;
+  return launched(dc::launch(append_fn(c->dtype, D, nm->interleaved != 0), dim3((unsigned)((warps + dc::APPEND_WARPS - 1) / dc::APPEND_WARPS)), dc::APPEND_WARPS * 32, 0, 1,
+                             (cudaStream_t)cuda_stream, &a), who);
 }
 
 extern "C" dc_status dc_cache_attend(dc_cache* c, const dc_token_batch* b, const void* q_dev, long long q_stride, float scale, void* out_dev,
