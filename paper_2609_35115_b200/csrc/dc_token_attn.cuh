@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   const int tl = threadIdx.x / G, hh = threadIdx.x % G;      // this row's token and head (warps 0 .. 3)
   const bool live = (int)threadIdx.x < n_rows;
   RowSet mine = any;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, m_odd, l_odd;
 
   if (warp == 4) {                                           // ---- copies
     if (ptx::elect_one()) {
@@ -215,15 +215,16 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
       if (j + 2 < n) ok = scores(j + 2);      // (into the columns that the product above has just read: products run in order)
     }
   } else {                                                   // ---- a query row per thread
-    // the queries, 16 bytes a lane, to the swizzled rows that the products read
+    // the queries to the swizzled rows that the products read, all copies in flight at once (a row at a time it took 9,000 cycles)
     constexpr int CPR = D / 8;
+    const uint32_t sq = ptx::smem_u32(sQ), inv_g = (65536u + G - 1) / G;      // r / G = r * inv_g >> 16 for r < 128, G <= 64
 #pragma unroll
     for (int i = 0; i < CPR; ++i) {
-      const int ch = i * 32 + lane, r = warp * 32 + ch / CPR, c = ch % CPR;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (r < n_rows) v = *reinterpret_cast<const uint4*>(Qg + (long long)(r / G) * a.q_stride + (r % G) * D + c * 8);
-      *reinterpret_cast<uint4*>(sQ + (c / 8) * QBOX + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+      const int ch = i * 32 + lane, r = warp * 32 + ch / CPR, c = ch % CPR, tr = (int)(r * inv_g >> 16);
+      const bool on = r < n_rows;
+      cp16(sq + (c / 8) * QBOX + r * 128 + (((c & 7) ^ (r & 7)) << 4), Qg + (on ? (long long)tr * a.q_stride + (r - tr * G) * D + c * 8 : 0), on);
     }
+    asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
     ptx::fence_proxy_async_smem();
     ptx::mbar_arrive(&bars.q_full);
     const int qp = q_lo + (live ? tl : 0);
@@ -320,21 +321,10 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   if (bars.failed) {
     ptx::pause_for_copies();
   } else if (warp < 4) {
-    const bool odd = bars.odd != 0;
     const uint32_t lane_base = tmem + ((uint32_t)warp << 21);
-    const T* q = Qg + (long long)(live ? tl : 0) * a.q_stride + (live ? hh : 0) * D;
     T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + (live ? tl : 0)) * a.out_stride + (long long)(kvh * G + (live ? hh : 0)) * D;
-    float* part = reinterpret_cast<float*>(sK);              // [128][D], 16-byte pieces of a row in the order piece ^ (row & 15)
-#pragma unroll 1
-    for (int c = 0; c < D; c += 16) {
-      float o[16];
-      if (n == 0) {
-        for (int i = 0; i < 16; ++i) o[i] = 0.f;
-      } else if (odd) {
-        plain_row<T, D>(a, q, Kg, Vg, mine, steps, n, m, c, o, c == 0 ? &m : nullptr, &l);
-      } else {
-        ptx::tmem_ld16(lane_base + CH_O + c, o);
-      }
+    float* part = reinterpret_cast<float*>(sK) + threadIdx.x * D;      // [128][D], 16-byte pieces of a row in the order piece ^ (row & 15)
+    auto emit = [&](int c, const float* o) {                           // 16 columns
       if (a.splits == 1) {
         const float inv = 1.0f / l;
         uint32_t w[8];
@@ -346,8 +336,31 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<float4*>(part + threadIdx.x * D + (((c / 4 + i) ^ (threadIdx.x & 15)) << 2)) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(part + (((c / 4 + i) ^ (threadIdx.x & 15)) << 2)) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+      }
+    };
+    if (n == 0) {
+      float o[16] = {};
+      for (int c = 0; c < D; c += 16) emit(c, o);
+    } else if (bars.odd) {
+      const T* q = Qg + (long long)(live ? tl : 0) * a.q_stride + (live ? hh : 0) * D;
+      float o[16];
+#pragma unroll 1
+      for (int c = 0; c < D; c += 16) {
+        plain_row<T, D>(a, q, Kg, Vg, mine, steps, n, m, c, o, c == 0 ? &m_odd : nullptr, &l_odd);
+        if (c == 0) {
+          m = m_odd;
+          l = l_odd;
+        }
+        emit(c, o);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < D; c += 64) {
+        float o[64];
+        ptx::tmem_ld64(lane_base + CH_O + c, o);
+#pragma unroll
+        for (int i = 0; i < 64; i += 16) emit(c + i, o + i);
       }
     }
     bars.m[threadIdx.x] = m;
@@ -359,25 +372,38 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   if (a.splits == 1) return;
   ptx::cluster_arrive();
   ptx::cluster_wait();
-  // join: the cluster's CTAs share the tile's elements out, four columns a thread
+  // join: the weight of every CTA's part in every row (over the queries' memory, which is done with), then the cluster's CTAs share the
+  // tile's elements out, four columns a thread
   const uint32_t part_s = ptx::smem_u32(sK), m_s = ptx::smem_u32(bars.m), l_s = ptx::smem_u32(bars.l);
-  for (int e = rank * CH_THREADS + threadIdx.x; e < n_rows * (D / 4); e += a.splits * CH_THREADS) {
-    const int r = e / (D / 4), c = e % (D / 4);
-    float M = -INFINITY;
-    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, ld_cluster(ptx::map_to_cta(m_s + r * 4, k)));
-    const float base = M == -INFINITY ? 0.f : M;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float L = 0.f;
+  float* weight = reinterpret_cast<float*>(sQ);      // [splits][128]
+  if ((int)threadIdx.x < n_rows) {
+    const int r = threadIdx.x;
+    float M = -INFINITY, L = 0.f;
 #pragma unroll 4
     for (int k = 0; k < a.splits; ++k) {
-      const float f = ex2(ld_cluster(ptx::map_to_cta(m_s + r * 4, k)) - base);
+      const float x = ld_cluster(ptx::map_to_cta(m_s + r * 4, k));
+      weight[k * CH_M + r] = x;
+      M = fmaxf(M, x);
+    }
+    const float base = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+    for (int k = 0; k < a.splits; ++k) L = fmaf(ex2(weight[k * CH_M + r] - base), ld_cluster(ptx::map_to_cta(l_s + r * 4, k)), L);
+    const float inv = 1.0f / L;
+    for (int k = 0; k < a.splits; ++k) weight[k * CH_M + r] = ex2(weight[k * CH_M + r] - base) * inv;
+  }
+  __syncthreads();
+#pragma unroll 2
+  for (int e = rank * CH_THREADS + threadIdx.x; e < n_rows * (D / 4); e += a.splits * CH_THREADS) {
+    const int r = e / (D / 4), c = e % (D / 4), tr = (int)(r * ((65536u + G - 1) / G) >> 16);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = 0; k < a.splits; ++k) {
+      const float f = weight[k * CH_M + r];
       const float4 v = ld_cluster4(ptx::map_to_cta(part_s + (r * D + ((c ^ (r & 15)) << 2)) * 4, k));
       o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));
-      L = fmaf(f, ld_cluster(ptx::map_to_cta(l_s + r * 4, k)), L);
     }
-    const float inv = 1.0f / L;
-    T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + r / G) * a.out_stride + (long long)(kvh * G + r % G) * D + c * 4;
-    *reinterpret_cast<uint2*>(out) = make_uint2(Num<T>::pack(o.x * inv, o.y * inv), Num<T>::pack(o.z * inv, o.w * inv));
+    T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + tr) * a.out_stride + (long long)(kvh * G + r - tr * G) * D + c * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(Num<T>::pack(o.x, o.y), Num<T>::pack(o.z, o.w));
   }
   ptx::cluster_arrive();      // no CTA's shared memory goes while another reads it
   ptx::cluster_wait();
