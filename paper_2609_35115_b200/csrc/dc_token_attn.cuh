@@ -245,17 +245,20 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
         // rows of V that nobody sees become zeros; of those that only some see, infinities and NaN are noted
         ok = warp_wait(&bars.v_full[st], (j / CH_STAGES) & 1);
         if (!ok) break;
+        // (half a row a thread; neighbouring rows' pieces lie in different banks)
+        const int r = threadIdx.x & (CH_N - 1), c0 = (int)(threadIdx.x / CH_N) * (CPR / 2);
+        uint8_t* row = sV + st * KVTILE + (c0 / 8) * KVBOX + r * 128;
         bool odd = false;
-#pragma unroll 1
-        for (int i = threadIdx.x; i < CH_N * CPR; i += CH_M) {
-          const int r = i / CPR, c = i % CPR;
-          if (in_all >> r & 1) continue;
-          uint4* p = reinterpret_cast<uint4*>(sV + st * KVTILE + (c / 8) * KVBOX + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-          if (in_any >> r & 1) {
-            const uint4 v = *p;
-            odd |= Num<T>::odd(v.x) | Num<T>::odd(v.y) | Num<T>::odd(v.z) | Num<T>::odd(v.w);
-          } else {
-            *p = make_uint4(0, 0, 0, 0);
+        if (!(in_all >> r & 1)) {
+#pragma unroll
+          for (int i = 0; i < CPR / 2; ++i) {
+            uint4* p = reinterpret_cast<uint4*>(row + (((((c0 & 7) + i) & 7) ^ (r & 7)) << 4));
+            if (in_any >> r & 1) {
+              const uint4 v = *p;
+              odd |= Num<T>::odd(v.x) | Num<T>::odd(v.y) | Num<T>::odd(v.z) | Num<T>::odd(v.w);
+            } else {
+              *p = make_uint4(0, 0, 0, 0);
+            }
           }
         }
         if (odd) bars.odd = 1;
@@ -375,35 +378,56 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   // join: the weight of every CTA's part in every row (over the queries' memory, which is done with), then the cluster's CTAs share the
   // tile's elements out, four columns a thread
   const uint32_t part_s = ptx::smem_u32(sK), m_s = ptx::smem_u32(bars.m), l_s = ptx::smem_u32(bars.l);
-  float* weight = reinterpret_cast<float*>(sQ);      // [splits][128]
+  // (a read from another CTA takes a thousand cycles: as many as fit are under way at once)
+  float *weight = reinterpret_cast<float*>(sQ), *sums = weight + 16 * CH_M;      // [splits][128]
+  for (int e = threadIdx.x; e < a.splits * CH_M; e += CH_THREADS) {
+    weight[e] = ld_cluster(ptx::map_to_cta(m_s + (e % CH_M) * 4, e / CH_M));
+    sums[e] = ld_cluster(ptx::map_to_cta(l_s + (e % CH_M) * 4, e / CH_M));
+  }
+  __syncthreads();
   if ((int)threadIdx.x < n_rows) {
     const int r = threadIdx.x;
     float M = -INFINITY, L = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < a.splits; ++k) {
-      const float x = ld_cluster(ptx::map_to_cta(m_s + r * 4, k));
-      weight[k * CH_M + r] = x;
-      M = fmaxf(M, x);
-    }
+    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, weight[k * CH_M + r]);
     const float base = M == -INFINITY ? 0.f : M;
-#pragma unroll 4
-    for (int k = 0; k < a.splits; ++k) L = fmaf(ex2(weight[k * CH_M + r] - base), ld_cluster(ptx::map_to_cta(l_s + r * 4, k)), L);
+    for (int k = 0; k < a.splits; ++k) L = fmaf(ex2(weight[k * CH_M + r] - base), sums[k * CH_M + r], L);
     const float inv = 1.0f / L;
     for (int k = 0; k < a.splits; ++k) weight[k * CH_M + r] = ex2(weight[k * CH_M + r] - base) * inv;
   }
   __syncthreads();
-#pragma unroll 2
-  for (int e = rank * CH_THREADS + threadIdx.x; e < n_rows * (D / 4); e += a.splits * CH_THREADS) {
-    const int r = e / (D / 4), c = e % (D / 4), tr = (int)(r * ((65536u + G - 1) / G) >> 16);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int k = 0; k < a.splits; ++k) {
-      const float f = weight[k * CH_M + r];
-      const float4 v = ld_cluster4(ptx::map_to_cta(part_s + (r * D + ((c ^ (r & 15)) << 2)) * 4, k));
-      o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));
+  const int total = n_rows * (D / 4), stride = a.splits * CH_THREADS;
+  for (int e0 = rank * CH_THREADS + threadIdx.x; e0 < total; e0 += 3 * stride) {
+    float4 o[3];
+#pragma unroll
+    for (int x = 0; x < 3; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < a.splits; k0 += 4) {
+      float4 v[3][4];
+#pragma unroll
+      for (int x = 0; x < 3; ++x)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int e = e0 + x * stride, r = e / (D / 4), c = e % (D / 4);
+          v[x][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (e < total && k0 + k < a.splits) v[x][k] = ld_cluster4(ptx::map_to_cta(part_s + (r * D + ((c ^ (r & 15)) << 2)) * 4, k0 + k));
+        }
+#pragma unroll
+      for (int x = 0; x < 3; ++x)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int e = e0 + x * stride;
+          if (e < total && k0 + k < a.splits) {
+            const float f = weight[(k0 + k) * CH_M + e / (D / 4)];
+            o[x] = make_float4(fmaf(f, v[x][k].x, o[x].x), fmaf(f, v[x][k].y, o[x].y), fmaf(f, v[x][k].z, o[x].z), fmaf(f, v[x][k].w, o[x].w));
+          }
+        }
     }
-    T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + tr) * a.out_stride + (long long)(kvh * G + r - tr * G) * D + c * 4;
-    *reinterpret_cast<uint2*>(out) = make_uint2(Num<T>::pack(o.x, o.y), Num<T>::pack(o.z, o.w));
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {
+      const int e = e0 + x * stride, r = e / (D / 4), c = e % (D / 4), tr = (int)(r * ((65536u + G - 1) / G) >> 16);
+      if (e >= total) break;
+      T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + tr) * a.out_stride + (long long)(kvh * G + r - tr * G) * D + c * 4;
+      *reinterpret_cast<uint2*>(out) = make_uint2(Num<T>::pack(o[x].x, o[x].y), Num<T>::pack(o[x].z, o[x].w));
+    }
   }
   ptx::cluster_arrive();      // no CTA's shared memory goes while another reads it
   ptx::cluster_wait();
