@@ -45,11 +45,10 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
       "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
-__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void st_cluster4(uint32_t addr, const float* v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
 }
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
 
 // The bounded wait (about a second) of a warp: all lanes agree on its outcome, so that what the warp does together stays together.
 constexpr uint32_t CH_POLLS = 1u << 18;
@@ -321,29 +320,38 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
     *a.err = 1;
   }
   __syncthreads();                                           // every product of this CTA has completed, or a wait has given up
-  if (bars.failed) {
-    ptx::pause_for_copies();
-  } else if (warp < 4) {
+  const bool failed = bars.failed != 0;
+  if (failed) ptx::pause_for_copies();
+  if (a.splits > 1) {      // every CTA of the cluster is through with its K and V: the parts go there
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  }
+  // Split tiles: CTA k finishes `own` rows from k * own on, and the others write their parts of those straight into its memory, [CTA][own][D] with the
+  // 16-byte pieces of a row in the order piece ^ (row & 15).  (Writes are posted; reading the parts from the other CTAs took 8,000 cycles of a full tile, a
+  // thousand a round.)
+  const int own = (n_rows + a.splits - 1) / a.splits;
+  const uint32_t part_s = ptx::smem_u32(sK);
+  if (warp < 4 && !failed) {
     const uint32_t lane_base = tmem + ((uint32_t)warp << 21);
     T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + (live ? tl : 0)) * a.out_stride + (long long)(kvh * G + (live ? hh : 0)) * D;
-    float* part = reinterpret_cast<float*>(sK) + threadIdx.x * D;      // [128][D], 16-byte pieces of a row in the order piece ^ (row & 15)
+    const int to = live ? threadIdx.x / own : 0, slot = rank * own + (live ? threadIdx.x % own : 0);
+    const uint32_t part = a.splits > 1 ? ptx::map_to_cta(part_s + slot * D * 4, to) : 0;
     auto emit = [&](int c, const float* o) {                           // 16 columns
+      if (!live) return;
       if (a.splits == 1) {
         const float inv = 1.0f / l;
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = Num<T>::pack(o[2 * i] * inv, o[2 * i + 1] * inv);
-        if (live) {
-          *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
-          *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-        }
+        *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(part + (((c / 4 + i) ^ (threadIdx.x & 15)) << 2)) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        for (int i = 0; i < 4; ++i) st_cluster4(part + (((c / 4 + i) ^ (slot & 15)) << 4), o + 4 * i);
       }
     };
     if (n == 0) {
-      float o[16] = {};
+      const float o[16] = {};
       for (int c = 0; c < D; c += 16) emit(c, o);
     } else if (bars.odd) {
       const T* q = Qg + (long long)(live ? tl : 0) * a.q_stride + (live ? hh : 0) * D;
@@ -366,69 +374,43 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
         for (int i = 0; i < 64; i += 16) emit(c + i, o + i);
       }
     }
-    bars.m[threadIdx.x] = m;
-    bars.l[threadIdx.x] = l;
+    if (a.splits > 1 && live) {
+      st_cluster(ptx::map_to_cta(ptx::smem_u32(&bars.m[slot]), to), m);
+      st_cluster(ptx::map_to_cta(ptx::smem_u32(&bars.l[slot]), to), l);
+    }
   }
   ptx::tc_fence_before();
   __syncthreads();
   if (warp == 5) ptx::tmem_dealloc(tmem, CH_TMEM);
   if (a.splits == 1) return;
   ptx::cluster_arrive();
-  ptx::cluster_wait();
-  // join: the weight of every CTA's part in every row (over the queries' memory, which is done with), then the cluster's CTAs share the
-  // tile's elements out, four columns a thread
-  const uint32_t part_s = ptx::smem_u32(sK), m_s = ptx::smem_u32(bars.m), l_s = ptx::smem_u32(bars.l);
-  // (a read from another CTA takes a thousand cycles: as many as fit are under way at once)
-  float *weight = reinterpret_cast<float*>(sQ), *sums = weight + 16 * CH_M;      // [splits][128]
-  for (int e = threadIdx.x; e < a.splits * CH_M; e += CH_THREADS) {
-    weight[e] = ld_cluster(ptx::map_to_cta(m_s + (e % CH_M) * 4, e / CH_M));
-    sums[e] = ld_cluster(ptx::map_to_cta(l_s + (e % CH_M) * 4, e / CH_M));
-  }
-  __syncthreads();
-  if ((int)threadIdx.x < n_rows) {
+  ptx::cluster_wait();      // (nobody reads or writes another CTA's memory behind this)
+  const int r0 = rank * own, mine_n = min(own, n_rows - r0);
+  float* weight = reinterpret_cast<float*>(sQ);      // [CTA][own]
+  if ((int)threadIdx.x < mine_n) {
     const int r = threadIdx.x;
     float M = -INFINITY, L = 0.f;
-    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, weight[k * CH_M + r]);
+    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, bars.m[k * own + r]);
     const float base = M == -INFINITY ? 0.f : M;
-    for (int k = 0; k < a.splits; ++k) L = fmaf(ex2(weight[k * CH_M + r] - base), sums[k * CH_M + r], L);
+    for (int k = 0; k < a.splits; ++k) L = fmaf(ex2(bars.m[k * own + r] - base), bars.l[k * own + r], L);
     const float inv = 1.0f / L;
-    for (int k = 0; k < a.splits; ++k) weight[k * CH_M + r] = ex2(weight[k * CH_M + r] - base) * inv;
+    for (int k = 0; k < a.splits; ++k) weight[k * own + r] = ex2(bars.m[k * own + r] - base) * inv;
   }
   __syncthreads();
-  const int total = n_rows * (D / 4), stride = a.splits * CH_THREADS;
-  for (int e0 = rank * CH_THREADS + threadIdx.x; e0 < total; e0 += 3 * stride) {
-    float4 o[3];
-#pragma unroll
-    for (int x = 0; x < 3; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = 0; k0 < a.splits; k0 += 4) {
-      float4 v[3][4];
-#pragma unroll
-      for (int x = 0; x < 3; ++x)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int e = e0 + x * stride, r = e / (D / 4), c = e % (D / 4);
-          v[x][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (e < total && k0 + k < a.splits) v[x][k] = ld_cluster4(ptx::map_to_cta(part_s + (r * D + ((c ^ (r & 15)) << 2)) * 4, k0 + k));
-        }
-#pragma unroll
-      for (int x = 0; x < 3; ++x)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int e = e0 + x * stride;
-          if (e < total && k0 + k < a.splits) {
-            const float f = weight[(k0 + k) * CH_M + e / (D / 4)];
-            o[x] = make_float4(fmaf(f, v[x][k].x, o[x].x), fmaf(f, v[x][k].y, o[x].y), fmaf(f, v[x][k].z, o[x].z), fmaf(f, v[x][k].w, o[x].w));
-          }
-        }
+  const float* parts = reinterpret_cast<const float*>(sK);
+  T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0) * a.out_stride + (long long)kvh * G * D;
+  constexpr int QUADS = D / 4;
+#pragma unroll 4
+  for (int e = threadIdx.x; e < mine_n * QUADS; e += CH_THREADS) {
+    const int r = e / QUADS, c = e % QUADS, row = r0 + r, tr = (int)(row * ((65536u + G - 1) / G) >> 16);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    int slot = r;
+#pragma unroll 2
+    for (int k = 0; k < a.splits; ++k, slot += own) {
+      const float f = weight[slot];
+      const float4 v = *reinterpret_cast<const float4*>(parts + slot * D + ((c ^ (slot & 15)) << 2));
+      o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));
     }
-#pragma unroll
-    for (int x = 0; x < 3; ++x) {
-      const int e = e0 + x * stride, r = e / (D / 4), c = e % (D / 4), tr = (int)(r * ((65536u + G - 1) / G) >> 16);
-      if (e >= total) break;
-      T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + tr) * a.out_stride + (long long)(kvh * G + r - tr * G) * D + c * 4;
-      *reinterpret_cast<uint2*>(out) = make_uint2(Num<T>::pack(o[x].x, o[x].y), Num<T>::pack(o[x].z, o[x].w));
-    }
+    *reinterpret_cast<uint2*>(out + (long long)tr * a.out_stride + (row - tr * G) * D + c * 4) = make_uint2(Num<T>::pack(o.x, o.y), Num<T>::pack(o.z, o.w));
   }
-  ptx::cluster_arrive();      // no CTA's shared memory goes while another reads it
-  ptx::cluster_wait();
 }
