@@ -18,7 +18,8 @@
 namespace dc {
 namespace {
 
-constexpr int SMP_THREADS = 256, SMP_WARPS = SMP_THREADS / 32;
+constexpr int SMP_THREADS = 256, SMP_WIDE = 512;      // threads of a CTA: rows in shared memory, rows that are streamed
+constexpr int SMP_WARPS = SMP_WIDE / 32;                // at most
 constexpr int SMP_BINS = 1024;
 constexpr int SMP_SLICE = 8192;           // logits of a CTA, while 16 CTAs are enough (then up to twice as many)
 constexpr int SMP_MAX_CLUSTER = 16;
@@ -141,45 +142,93 @@ struct Cut {
 template <typename T>
 __device__ __forceinline__ float as_float(T x) { return (float)x; }
 
-// Loads the slice into shared memory and returns this thread's maximum.  16-byte vectors on their own alignment: the first
-// `shift` places of shared memory lie before the slice.  (NaN is left: it compares as false, like -infinity it is never kept.)
-template <typename T>
-__device__ __forceinline__ float load_slice(const T* src, int n, int shift, float* l) {
-  constexpr int VE = 16 / sizeof(T);
-  const int vectors = (shift + n + VE - 1) / VE;
-  float top = -INFINITY;
-#pragma unroll 4
-  for (int v = threadIdx.x; v < vectors; v += SMP_THREADS) {
-    const int at = v * VE - shift;
-    alignas(16) T x[VE];
-    if (at >= 0 && at + VE <= n) {
-      *reinterpret_cast<uint4*>(x) = __ldcs(reinterpret_cast<const uint4*>(src + at));
-    } else {
-#pragma unroll
-      for (int i = 0; i < VE; ++i) x[i] = at + i >= 0 && at + i < n ? src[at + i] : (T)-INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < VE; i += 4) {
-      const float4 y = make_float4(as_float(x[i]), as_float(x[i + 1]), as_float(x[i + 2]), as_float(x[i + 3]));
-      top = fmaxf(fmaxf(top, fmaxf(y.x, y.y)), fmaxf(y.z, y.w));
-      *reinterpret_cast<float4*>(l + v * VE + i) = y;
-    }
-  }
-  return top;
-}
+// A CTA's slice of a row, as places: logit i of the slice is at place shift + i, where 16-byte vectors of the caller's memory begin at
+// multiples of their size.  Either the slice lies in shared memory, as fp32, or (STREAM) every pass reads the caller's memory, which the L2
+// cache holds behind the first.  NaN is left: it compares as false, like -infinity it is never kept.
+template <typename T, bool STREAM, int NT>
+struct Row {
+  static constexpr int VE = 16 / sizeof(T);
+  const T* src;       // place 0
+  int      shift, end, places;      // the slice is [shift, end); places: whole steps of all warps
+  float*   l;
+  bool     infinite;  // +infinity is the largest: it counts as 0, everything finite as -infinity
 
-// Calls f(logit) for every logit of this thread's share of the slice.
-template <typename F>
-__device__ __forceinline__ void each_logit(const float* l, int places, F f) {
-#pragma unroll 2
-  for (int i = threadIdx.x * 4; i < places; i += SMP_THREADS * 4) {
-    const float4 v = *reinterpret_cast<const float4*>(l + i);
-    f(v.x);
-    f(v.y);
-    f(v.z);
-    f(v.w);
+  // STREAM: four places from the caller's memory
+  __device__ __forceinline__ float4 from_memory(int i) const {
+    float4 y;
+    if (i >= shift && i + 4 <= end) {
+      if (sizeof(T) == 4) {
+        y = *reinterpret_cast<const float4*>(src + i);
+      } else {
+        alignas(8) T x[4];
+        *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(src + i);
+        y = make_float4(as_float(x[0]), as_float(x[1]), as_float(x[2]), as_float(x[3]));
+      }
+    } else {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = i + e >= shift && i + e < end ? as_float(src[i + e]) : -INFINITY;
+      y = make_float4(x[0], x[1], x[2], x[3]);
+    }
+    return y;
   }
-}
+  static __device__ __forceinline__ float against_infinity(float x) { return x == INFINITY ? 0.f : -INFINITY; }
+  __device__ __forceinline__ float4 quad(int i) const {
+    if (!STREAM) return *reinterpret_cast<const float4*>(l + i);
+    float4 y = from_memory(i);
+    if (infinite) y = make_float4(against_infinity(y.x), against_infinity(y.y), against_infinity(y.z), against_infinity(y.w));
+    return y;
+  }
+  // Calls f(place, four logits) for this thread's share of the slice; several loads are under way at once.
+  template <typename F>
+  __device__ __forceinline__ void each_quad(F f) const {
+    constexpr int U = STREAM ? 4 : 2;
+    for (int i0 = threadIdx.x * 4; i0 < places; i0 += U * NT * 4) {
+      float4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * NT * 4 < places) v[u] = quad(i0 + u * NT * 4);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i0 + u * NT * 4 < places) f(i0 + u * NT * 4, v[u]);
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each_logit(F f) const {
+    each_quad([&](int, const float4& v) {
+      f(v.x);
+      f(v.y);
+      f(v.z);
+      f(v.w);
+    });
+  }
+  // This thread's maximum; fills shared memory.
+  __device__ __forceinline__ float load() const {
+    float top = -INFINITY;
+    if constexpr (STREAM) {
+      each_quad([&](int, const float4& y) { top = fmaxf(fmaxf(top, fmaxf(y.x, y.y)), fmaxf(y.z, y.w)); });
+    } else {
+#pragma unroll 4
+      for (int at = threadIdx.x * VE; at < end; at += NT * VE) {
+        alignas(16) T x[VE];
+        if (at >= shift && at + VE <= end) {
+          *reinterpret_cast<uint4*>(x) = __ldcs(reinterpret_cast<const uint4*>(src + at));
+        } else {
+#pragma unroll
+          for (int i = 0; i < VE; ++i) x[i] = at + i >= shift && at + i < end ? src[at + i] : (T)-INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) {
+          const float4 y = make_float4(as_float(x[i]), as_float(x[i + 1]), as_float(x[i + 2]), as_float(x[i + 3]));
+          top = fmaxf(fmaxf(top, fmaxf(y.x, y.y)), fmaxf(y.z, y.w));
+          *reinterpret_cast<float4*>(l + at + i) = y;
+        }
+      }
+      for (int i = (end + VE - 1) / VE * VE + threadIdx.x; i < places; i += NT) l[i] = -INFINITY;
+    }
+    return top;
+  }
+};
 
 // Bins of a row.  Selection needs bins that fall with the logit and spread the row's logits, so that few of a warp's lanes meet in one:
 // 22 to a factor of two of weight, then 1024 in each of those, by fp32 arithmetic (each operation is monotone, and the
@@ -209,12 +258,12 @@ __device__ __forceinline__ void add_to_bin(unsigned long long* bin, const Weigh&
 
 // Finds the bin of the cluster's histograms in which `over` plus the running sum, from bin 0 up (DOWN: from the last bin down), reaches
 // target(total): groups of bins first, then the group's bins, so that little is read from the other CTAs.
-template <bool DOWN, typename F>
+template <bool DOWN, int NT, typename F>
 __device__ __forceinline__ bool find_bin(SampleShared& sh, int buf, unsigned long long over, F target_of, int splits) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __syncthreads();
 #pragma unroll
-  for (int g = warp * (SMP_GROUPS / SMP_WARPS); g < (warp + 1) * (SMP_GROUPS / SMP_WARPS); ++g) {
+  for (int g = warp; g < SMP_GROUPS; g += NT / 32) {
     const unsigned long long s = warp_sum(sh.hist[buf][g * 32 + lane]);
     if (lane == 0) sh.group[buf][g] = s;
   }
@@ -262,19 +311,19 @@ __device__ __forceinline__ bool find_bin(SampleShared& sh, int buf, unsigned lon
 // Selection over the cluster: the key at which the running count (BY_MASS: mass) of the descending order reaches the target, among the
 // logits from `low` up; what lies above it, what it holds itself, and the target are left in `sh`.  False if the whole of it does not
 // reach the target.  `buf` alternates: a buffer is cleared two rounds after it was filled, when every CTA has read it.
-template <bool BY_MASS, typename F>
-__device__ __forceinline__ bool select(SampleShared& sh, const float* l, int places, const Weigh& w, const Binned& bins, float low, F target_of, int splits, int& buf, uint32_t* key) {
+template <bool BY_MASS, typename T, bool STREAM, int NT, typename F>
+__device__ __forceinline__ bool select(SampleShared& sh, const Row<T, STREAM, NT>& row, const Weigh& w, const Binned& bins, float low, F target_of, int splits, int& buf, uint32_t* key) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   auto clear = [&] {
-    for (int i = tid; i < SMP_BINS; i += SMP_THREADS) sh.hist[buf][i] = 0;
+    for (int i = tid; i < SMP_BINS; i += NT) sh.hist[buf][i] = 0;
     __syncthreads();
   };
   clear();
-  each_logit(l, places, [&](float x) {
+  row.each_logit([&](float x) {
     const float t = bins.place(x);
     if (x >= low) add_to_bin<BY_MASS>(&sh.hist[buf][(int)t], w, x);
   });
-  const bool found = find_bin<false>(sh, buf, 0, target_of, splits);
+  const bool found = find_bin<false, NT>(sh, buf, 0, target_of, splits);
   buf ^= 1;
   if (!found) return false;
   const int b0 = sh.bin;
@@ -287,12 +336,12 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   if (x_lo > low) x_lo = logit_of(key_of(x_lo) - 2);
   if (x_hi < x_top) x_hi = logit_of(key_of(x_hi) + 2);
   clear();
-  each_logit(l, places, [&](float x) {
+  row.each_logit([&](float x) {
     if (!(x >= x_lo && x <= x_hi)) return;
     const float t = bins.place(x);
     if (x >= low && (int)t == b0) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
   });
-  find_bin<false>(sh, buf, above, known, splits);
+  find_bin<false, NT>(sh, buf, above, known, splits);
   buf ^= 1;
   const int b1 = sh.bin;
   auto in_bin = [&](float x) {
@@ -302,7 +351,7 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   };
   // one logit, as a rule, or equal ones: the bin's smallest and largest key (the latter inverted)
   uint32_t lo = 0xffffffffu, hi = 0xffffffffu;
-  each_logit(l, places, [&](float x) {
+  row.each_logit([&](float x) {
     if (in_bin(x)) {
       lo = min(lo, key_of(x));
       hi = min(hi, ~key_of(x));
@@ -312,7 +361,7 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   hi = __reduce_min_sync(0xffffffffu, hi);
   if (lane == 0) sh.warp_sum[warp] = (unsigned long long)hi << 32 | lo;
   __syncthreads();
-  for (int i = 0; i < SMP_WARPS; ++i) {
+  for (int i = 0; i < NT / 32; ++i) {
     lo = min(lo, (uint32_t)sh.warp_sum[i]);
     hi = min(hi, (uint32_t)(sh.warp_sum[i] >> 32));
   }
@@ -334,11 +383,11 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
     const int shift = 22 - 10 * level > 0 ? 22 - 10 * level : 0, bits = level == 3 ? 2 : 10;
     above = sh.above;
     clear();
-    each_logit(l, places, [&](float x) {
+    row.each_logit([&](float x) {
       const uint32_t k = key_of(x);
       if (in_bin(x) && (level == 0 || k >> (shift + bits) == prefix)) add_to_bin<BY_MASS>(&sh.hist[buf][k >> shift & ((1u << bits) - 1)], w, x);
     });
-    find_bin<true>(sh, buf, above, known, splits);
+    find_bin<true, NT>(sh, buf, above, known, splits);
     buf ^= 1;
     prefix = prefix << bits | (uint32_t)sh.bin;
   }
@@ -346,27 +395,31 @@ __device__ __forceinline__ bool select(SampleShared& sh, const float* l, int pla
   return true;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs a) {
+template <typename T, bool STREAM>
+__global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 4) sample_kernel(const SampleArgs a) {
+  constexpr int NT = STREAM ? SMP_WIDE : SMP_THREADS, WARPS = NT / 32;
   extern __shared__ __align__(16) float l[];
   __shared__ SampleShared sh;
   ptx::pdl_wait();
   ptx::pdl_launch();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x, row = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x, row_i = blockIdx.y;
   const int from = min(a.vocab, rank * a.slice), n = min(a.vocab, from + a.slice) - from;
-  const T* src = static_cast<const T*>(a.logits) + (long long)row * a.stride + from;
-  const int shift = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
-  const float temperature = a.temperature ? a.temperature[row] : 1.f, top_p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f, u = a.u[row];
-  const int top_k = a.top_k ? a.top_k[row] : 0;
-  const bool greedy = !(temperature > 0.f) || top_k == 1;
-
-  float top = load_slice(src, n, shift, l);
-  sh.table[tid] = exp2_table.v[tid];
+  const T* first = static_cast<const T*>(a.logits) + (long long)row_i * a.stride + from;
+  Row<T, STREAM, NT> row;
+  row.shift = (int)((reinterpret_cast<uintptr_t>(first) & 15) / sizeof(T));
+  row.src = first - row.shift;
+  row.end = row.shift + n;
+  row.l = l;
+  row.infinite = false;
   // a warp's part of the slice is contiguous: what is summed in the vocabulary's order is summed by warps, in steps of 128
-  constexpr int STEP = 128, VE = 16 / sizeof(T);
-  const int filled = (shift + n + VE - 1) / VE * VE;
-  const int part = (filled + SMP_WARPS * STEP - 1) / (SMP_WARPS * STEP) * STEP, places = part * SMP_WARPS;
-  for (int i = filled + tid; i < places; i += SMP_THREADS) l[i] = -INFINITY;
+  constexpr int STEP = 128;
+  const int part = (row.end + WARPS * STEP - 1) / (WARPS * STEP) * STEP, index0 = from - row.shift;
+  row.places = part * WARPS;
+  const float temperature = a.temperature ? a.temperature[row_i] : 1.f, top_p = a.top_p ? a.top_p[row_i] : 1.f, min_p = a.min_p ? a.min_p[row_i] : 0.f, u = a.u[row_i];
+  const int top_k = a.top_k ? a.top_k[row_i] : 0;
+  const bool greedy = !(temperature > 0.f) || top_k == 1;
+  float top = row.load();
+  if (tid < 256) sh.table[tid] = exp2_table.v[tid];
 
   // ---- the largest logit -----------------------------------------------------------------------------------------------------
 #pragma unroll
@@ -374,20 +427,19 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
   if (lane == 0) sh.warp_sum[warp] = __float_as_uint(top);
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < SMP_WARPS; ++i) top = fmaxf(top, __uint_as_float((uint32_t)sh.warp_sum[i]));
+  for (int i = 0; i < WARPS; ++i) top = fmaxf(top, __uint_as_float((uint32_t)sh.warp_sum[i]));
   unsigned long long best = (unsigned long long)key_of(top) << 32;
   if (greedy) {      // and its first place
     uint32_t at = 0xffffffffu;
-    for (int i = tid * 4; i < places; i += SMP_THREADS * 4) {
-      const float4 v = *reinterpret_cast<const float4*>(l + i);
+    row.each_quad([&](int i, const float4& v) {
       const uint32_t e = v.x == top ? 0 : v.y == top ? 1 : v.z == top ? 2 : v.w == top ? 3 : 4;
-      if (e < 4) at = min(at, (uint32_t)(from - shift + i) + e);
-    }
+      if (e < 4) at = min(at, (uint32_t)(index0 + i) + e);
+    });
     at = __reduce_min_sync(0xffffffffu, at);
     if (lane == 0) sh.warp_ties[warp] = at;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < SMP_WARPS; ++i) at = min(at, sh.warp_ties[i]);
+    for (int i = 0; i < WARPS; ++i) at = min(at, sh.warp_ties[i]);
     best |= (uint32_t)~at;
   }
   if (a.splits > 1) {
@@ -402,15 +454,17 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
   const uint32_t best_key = (uint32_t)(best >> 32);
   if (greedy || best_key <= KEY_NONE) {
     if (rank == 0 && tid == 0) {
-      a.tokens[row] = best_key <= KEY_NONE ? -1 : (int)~(uint32_t)best;
-      if (a.probs) a.probs[row] = best_key <= KEY_NONE ? 0.f : 1.f;
+      a.tokens[row_i] = best_key <= KEY_NONE ? -1 : (int)~(uint32_t)best;
+      if (a.probs) a.probs[row_i] = best_key <= KEY_NONE ? 0.f : 1.f;
     }
     if (a.splits > 1) cluster_or_block_sync(a.splits);      // no CTA's shared memory goes while another reads it
     return;
   }
   top = logit_of(best_key);
   if (isinf(top)) {      // +infinity outweighs everything finite: as zeros against nothing
-    for (int i = tid; i < places; i += SMP_THREADS) l[i] = l[i] == INFINITY ? 0.f : -INFINITY;
+    row.infinite = true;
+    if (!STREAM)
+      for (int i = tid; i < row.places; i += NT) l[i] = row.against_infinity(l[i]);
     top = 0.f;
     __syncthreads();
   }
@@ -431,7 +485,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
   int buf = 0;
   uint32_t key;
   unsigned long long too_many = 0;      // ties that top-k leaves out
-  if (top_k > 0 && top_k < a.vocab && select<false>(sh, l, places, w, bins, cut.low, [&](unsigned long long) { return (unsigned long long)top_k; }, a.splits, buf, &key)) {
+  if (top_k > 0 && top_k < a.vocab && select<false>(sh, row, w, bins, cut.low, [&](unsigned long long) { return (unsigned long long)top_k; }, a.splits, buf, &key)) {
     too_many = sh.inside - (top_k - sh.above);
     cut_at(key, top_k - sh.above, too_many == 0);
   }
@@ -444,7 +498,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
       const unsigned long long target = want >= 1.0 ? (unsigned long long)want : 1ull;
       return target < mass ? target : mass;
     };
-    if (select<true>(sh, l, places, w, bins, cut.ties ? cut.tie : cut.low, part_of, a.splits, buf, &key)) {
+    if (select<true>(sh, row, w, bins, cut.ties ? cut.tie : cut.low, part_of, a.splits, buf, &key)) {
       const unsigned long long each = w.fixed(logit_of(key)), ties = (sh.target - sh.above + each - 1) / each;
       cut_at(key, ties, ties * each == sh.inside);
     }
@@ -472,7 +526,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
   if (cut.ties) {
     uint32_t mine = 0;
     for (int i = warp * part + lane * 4; i < (warp + 1) * part; i += STEP) {
-      const float4 v = *reinterpret_cast<const float4*>(l + i);
+      const float4 v = row.quad(i);
       mine += (v.x == cut.tie) + (v.y == cut.tie) + (v.z == cut.tie) + (v.w == cut.tie);
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
@@ -480,7 +534,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
     __syncthreads();
     if (tid == 0) {
       uint32_t all = 0;
-      for (int i = 0; i < SMP_WARPS; ++i) all += sh.warp_ties[i];
+      for (int i = 0; i < WARPS; ++i) all += sh.warp_ties[i];
       sh.ties = all;
     }
     if (a.splits > 1) {
@@ -490,8 +544,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
     for (int i = 0; i < warp; ++i) ties_before += sh.warp_ties[i];
   }
   // The weights of four neighbouring places, of kept tokens only; `seen`: the cut's ties in front of this step.
-  auto weights = [&](int i, unsigned long long& seen, unsigned long long* m) {
-    const float4 v = *reinterpret_cast<const float4*>(l + i);
+  auto weights = [&](const float4& v, unsigned long long& seen, unsigned long long* m) {
     const float x[4] = {v.x, v.y, v.z, v.w};
     bool on[4];
 #pragma unroll
@@ -525,10 +578,17 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
 
   // ---- the draw: running mass in the vocabulary's order ------------------------------------------------------------------------------
   unsigned long long seen = ties_before, sum = 0;
-  for (int i = warp * part + lane * 4; i < (warp + 1) * part; i += STEP) {
-    unsigned long long m[4];
-    weights(i, seen, m);
-    sum += (m[0] + m[1]) + (m[2] + m[3]);
+  constexpr int U = STREAM ? 4 : 2;      // steps whose loads are under way at once
+  for (int i0 = warp * part + lane * 4; i0 < (warp + 1) * part; i0 += U * STEP) {
+    float4 v[U];
+#pragma unroll
+    for (int x = 0; x < U; ++x) v[x] = i0 + x * STEP < (warp + 1) * part ? row.quad(i0 + x * STEP) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+#pragma unroll
+    for (int x = 0; x < U; ++x) {
+      unsigned long long m[4];
+      weights(v[x], seen, m);
+      sum += (m[0] + m[1]) + (m[2] + m[3]);
+    }
   }
   sum = warp_sum(sum);
   __syncthreads();
@@ -536,7 +596,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
   __syncthreads();
   unsigned long long start = 0, mass = 0;
 #pragma unroll
-  for (int i = 0; i < SMP_WARPS; ++i) {
+  for (int i = 0; i < WARPS; ++i) {
     if (i < warp) start += sh.warp_sum[i];
     mass += sh.warp_sum[i];
   }
@@ -558,14 +618,15 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
     unsigned long long run = start;
     seen = ties_before;
     for (int i = warp * part + lane * 4; i < (warp + 1) * part; i += STEP) {
+      const float4 v = row.quad(i);
       unsigned long long m[4];
-      weights(i, seen, m);
+      weights(v, seen, m);
       const unsigned long long four = m[0] + m[1] + m[2] + m[3], upto = warp_scan(four, lane) + run, before = upto - four;
       if (target >= before && target < upto) {
         const unsigned long long in = target - before;
         const int e = in < m[0] ? 0 : in < m[0] + m[1] ? 1 : in < m[0] + m[1] + m[2] ? 2 : 3;
-        a.tokens[row] = from - shift + i + e;
-        if (a.probs) a.probs[row] = (float)(w.value(l[i + e]) / ((double)mass / (double)ONE));
+        a.tokens[row_i] = index0 + i + e;
+        if (a.probs) a.probs[row_i] = (float)(w.value(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) / ((double)mass / (double)ONE));
       }
       run = __shfl_sync(0xffffffffu, upto, 31);
       if (target < run) break;
@@ -574,21 +635,21 @@ __global__ void __launch_bounds__(SMP_THREADS, 4) sample_kernel(const SampleArgs
   if (a.splits > 1) cluster_or_block_sync(a.splits);
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 cudaError_t launch_sample(const SampleArgs& a, int rows, size_t smem, cudaStream_t st) {
   static thread_local int ready = -1;      // device that has the kernel's attributes
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess && ready != dev) {
-    e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (SMP_SLICE + SMP_WARPS * 128) * 4);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess && ready != dev && !STREAM) {
+    e = cudaFuncSetAttribute(sample_kernel<T, STREAM>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (SMP_SLICE + SMP_THREADS * 4) * 4);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<T, STREAM>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) ready = dev;
   }
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
   cfg.gridDim = dim3(a.splits, rows);
-  cfg.blockDim = dim3(SMP_THREADS);
+  cfg.blockDim = dim3(STREAM ? SMP_WIDE : SMP_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -598,7 +659,11 @@ cudaError_t launch_sample(const SampleArgs& a, int rows, size_t smem, cudaStream
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.splits > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a);
+  return cudaLaunchKernelEx(&cfg, sample_kernel<T, STREAM>, a);
+}
+template <typename T>
+cudaError_t launch_rows(const SampleArgs& a, int rows, size_t smem, bool stream, cudaStream_t st) {
+  return stream ? launch_sample<T, true>(a, rows, 0, st) : launch_sample<T, false>(a, rows, smem, st);
 }
 
 }  // namespace
@@ -632,14 +697,19 @@ extern "C" dc_status dc_sample_tokens(const void* logits_dev, int dtype, int n_r
     return DC_ERR_CUDA;
   }
   SampleArgs a{logits_dev, row_stride, vocab, 0, 1, rules->temperature_dev, rules->top_p_dev, rules->min_p_dev, u_dev, rules->top_k_dev, tokens_dev, probs_dev};
-  // CTAs of a row: as many as its logits need, and while SMs are idle more, down to 4096 logits each.
-  while (a.splits < SMP_MAX_CLUSTER && (long long)a.splits * SMP_SLICE < vocab) a.splits *= 2;
-  while (a.splits < SMP_MAX_CLUSTER && (long long)n_rows * a.splits * 2 <= n_sm && vocab / a.splits > 4096) a.splits *= 2;
+  // Rows enough for every SM: a CTA streams its row.  Else the row lies in the shared memory of a cluster: as many CTAs as its logits need, and while SMs are
+  // idle more, down to 4096 logits each.
+  const bool stream = n_rows >= n_sm && vocab > SMP_SLICE;
+  if (!stream) {
+    while (a.splits < SMP_MAX_CLUSTER && (long long)a.splits * SMP_SLICE < vocab) a.splits *= 2;
+    while (a.splits < SMP_MAX_CLUSTER && (long long)n_rows * a.splits * 2 <= n_sm && vocab / a.splits > 4096) a.splits *= 2;
+  }
   a.slice = ((vocab + a.splits - 1) / a.splits + 7) & ~7;
-  const int filled = (a.slice + 7 + 7) & ~7, part = (filled + SMP_WARPS * 128 - 1) / (SMP_WARPS * 128) * 128;
-  const size_t smem = (size_t)part * SMP_WARPS * 4;
+  const int part = (a.slice + 7 + SMP_THREADS * 4 - 1) / (SMP_THREADS * 4) * (SMP_THREADS * 4);
+  const size_t smem = (size_t)part * 4;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  e = dtype == DC_F32 ? launch_sample<float>(a, n_rows, smem, st) : dtype == DC_BF16 ? launch_sample<__nv_bfloat16>(a, n_rows, smem, st) : launch_sample<__half>(a, n_rows, smem, st);
+  e = dtype == DC_F32 ? launch_rows<float>(a, n_rows, smem, stream, st)
+                      : dtype == DC_BF16 ? launch_rows<__nv_bfloat16>(a, n_rows, smem, stream, st) : launch_rows<__half>(a, n_rows, smem, stream, st);
   if (e != cudaSuccess) {
     cudaGetLastError();      // (a refused launch leaves its code behind)
     set_error("dc_sample_tokens: launch failed: %s", cudaGetErrorString(e));

@@ -234,3 +234,29 @@ def test_scores_closer_than_weights_can_tell(dc, T):
     l[:, ::3] *= 1e38
     l[0, 7], l[0, 8] = torch.finfo(torch.float32).max, torch.finfo(torch.float32).min
     check(dc, l, u, T=np.full(n, T), k=1 + np.arange(n) * 1700, p=np.full(n, 0.8))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,stride", [(8200, 8200), (9001, 9003), (30000, 30002)])
+def test_many_rows(dc, vocab, stride, dtype):
+    """Rows enough for every SM: a row is streamed by one CTA."""
+    t = TYPES[dtype]
+    rng = np.random.default_rng(vocab)
+    n = 150
+    wide = logits_of(rng, n, stride, t)
+    wide[:, vocab:] = 60.0
+    l = wide[:, :vocab]
+    u = rng.random(n)
+    r = np.arange(n)
+    check(dc, l, u, T=np.where(r % 7 == 6, 0.0, 0.4 + 0.02 * r), k=np.where(r % 3 == 0, 0, 5 * r), p=np.where(r % 4 == 0, 1.0, 0.3 + 0.004 * r), m=np.where(r % 5 == 0, 0.0, 0.001 * r))
+    l[:40] = torch.tensor(rng.integers(-4, 3, (40, vocab)) * 0.5, device="cuda").to(t)      # ties
+    l[40:50] = 1.0
+    l[50] = -torch.inf
+    l[51, : vocab - 1] = torch.nan
+    l[52:56, 3::7] = torch.inf
+    l[56:60, ::2] = -torch.inf
+    l[60], l[61] = torch.finfo(t).max, torch.finfo(t).min
+    l[62:66, 5:] = -torch.inf
+    check(dc, l, u, T=0.5 + 0.01 * r, k=np.where(r % 2 == 0, 0, 1 + r * vocab // 300), p=np.where(r % 4 < 2, 1.0, (r + 1) / 151))
+    check(dc, l, u, p=np.full(n, 0.5), T=np.where(r % 2 == 0, 1e30, 0.7))
+    check(dc, l, u, T=np.zeros(n))
