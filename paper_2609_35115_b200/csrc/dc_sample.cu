@@ -52,7 +52,9 @@ struct SampleShared {
   float              at_least;               // by mass: the logits in it and above are no fewer
   uint32_t           warp_ties[SMP_WARPS];
   uint32_t           ties;                   // of the slice
-  uint32_t           few;                    // candidates of the slice
+  uint32_t           few;                    // collected logits of the slice
+  uint32_t           found;                  // key of a selection among few, and what lies above it
+  unsigned long long found_above;
   int                bin;
 };
 
@@ -318,6 +320,31 @@ __device__ __forceinline__ bool find_bin(SampleShared& sh, int buf, unsigned lon
   return sh.bin >= 0;      // (all of this is written anew behind a barrier that everyone passes)
 }
 
+// The words that the cluster's CTAs have collected, one CTA's behind the other's.  `count`: CTA `lane`'s number of them; n in all.
+// (A read from another CTA takes a thousand cycles: all are under way at once.)
+template <int NT>
+__device__ __forceinline__ void pull_few(unsigned long long* to, const unsigned long long* collected, uint32_t count, int n, int splits) {
+  const int lane = threadIdx.x & 31;
+  uint32_t upto = count;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += y;
+  }
+  for (int i0 = 0; i0 < n; i0 += NT) {
+    const int i = i0 + (int)threadIdx.x;
+    int k = 0, before = 0;
+    for (int x = 0; x < splits - 1; ++x) {
+      const int end = (int)__shfl_sync(0xffffffffu, upto, x);
+      if (i >= end) {
+        k = x + 1;
+        before = end;
+      }
+    }
+    if (i < n) to[i] = ld_cluster64(ptx::map_to_cta(ptx::smem_u32(collected + (i - before)), k));
+  }
+}
+
 // Selection over the cluster: the key at which the running count (BY_MASS: mass) of the descending order reaches the target, among the
 // logits from `low` up; what lies above it, what it holds itself, and the target are left in `sh`.  False if the whole of it does not
 // reach the target.  `buf` alternates: a buffer is cleared two rounds after it was filled, when every CTA has read it.
@@ -405,12 +432,16 @@ __device__ __forceinline__ Selected select(SampleShared& sh, const Row<T, STREAM
     const float t = bins.place(x);
     return x >= low && (int)t == b0 && Binned::inner(t, b0) == b1;
   };
-  // one logit, as a rule, or equal ones: the bin's smallest and largest key (the latter inverted)
+  // one logit, as a rule, or equal ones, or a few: each CTA collects its own, with the bin's smallest and largest key (the latter inverted)
   uint32_t lo = 0xffffffffu, hi = 0xffffffffu;
+  if (tid == 0) sh.few = 0;
+  __syncthreads();
   row.each_logit([&](float x) {
     if (in_bin(x)) {
       lo = min(lo, key_of(x));
       hi = min(hi, ~key_of(x));
+      const uint32_t at = atomicAdd(&sh.few, 1u);
+      if (at < SMP_FEW) sh.hist[buf][at] = key_of(x);
     }
   });
   lo = __reduce_min_sync(0xffffffffu, lo);
@@ -421,19 +452,50 @@ __device__ __forceinline__ Selected select(SampleShared& sh, const Row<T, STREAM
     lo = min(lo, (uint32_t)sh.warp_sum[i]);
     hi = min(hi, (uint32_t)(sh.warp_sum[i] >> 32));
   }
+  uint32_t count = sh.few, n = count;
   if (splits > 1) {
     if (tid == 0) sh.range[BY_MASS] = (unsigned long long)hi << 32 | lo;
     cluster_or_block_sync(splits);
+    count = 0;
     if (lane < splits) {
       const unsigned long long x = ld_cluster64(ptx::map_to_cta(ptx::smem_u32(&sh.range[BY_MASS]), lane));
+      count = ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few), lane));
       lo = min(lo, (uint32_t)x);
       hi = min(hi, (uint32_t)(x >> 32));
     }
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_min_sync(0xffffffffu, hi);
+    n = __reduce_add_sync(0xffffffffu, count);
   }
   *key = lo;
   if (lo == ~hi) return SELECT_KEY;
+  if (n <= SMP_FEW) {      // every CTA takes them all and finds the same
+    unsigned long long *c = sh.hist[buf ^ 1], *mass = sh.hist[buf ^ 1] + SMP_FEW;
+    pull_few<NT>(c, sh.hist[buf], splits > 1 ? count : lane == 0 ? n : 0, (int)n, splits);
+    buf ^= 1;              // (the collected ones stay as they are until the next histogram's barrier)
+    __syncthreads();
+    const uint32_t me = tid < (int)n ? (uint32_t)c[tid] : 0;
+    if (tid < (int)n) mass[tid] = BY_MASS ? w.fixed(logit_of(me)) : 1ull;
+    __syncthreads();
+    if (tid < (int)n) {
+      unsigned long long over = sh.above, same = 0;
+      for (uint32_t i = 0; i < n; ++i) {
+        const uint32_t k = (uint32_t)c[i];
+        if (k > me) over += mass[i];
+        if (k == me) same += mass[i];
+      }
+      if (over < target && over + same >= target) {      // (equal logits write the same)
+        sh.found = me;
+        sh.found_above = over;
+        sh.inside = same;
+      }
+    }
+    __syncthreads();
+    *key = sh.found;
+    if (tid == 0) sh.above = sh.found_above;
+    __syncthreads();
+    return SELECT_KEY;
+  }
   // several logits share the bin (scores far closer to each other than weights can tell): by the bits of their keys
   uint32_t prefix = 0;
 #pragma unroll 1
@@ -597,27 +659,8 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
   if (got == SELECT_FEW) {
     unsigned long long *c = sh.hist[buf ^ 1], *sums = sh.hist[buf];      // (the first was read by everyone before the candidates' barrier; the second has the slice's own)
     if (rank == 0) {
-      // (a read from another CTA takes a thousand cycles: all counts at once, then all candidates)
       const uint32_t count = lane < a.splits ? ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few), lane)) : 0;
-      uint32_t upto = count;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += y;
-      }
-#pragma unroll 4
-      for (int i0 = 0; i0 < few; i0 += NT) {
-        const int i = i0 + tid;
-        int k = 0, before = 0;
-        for (int x = 0; x < a.splits - 1; ++x) {
-          const int end = (int)__shfl_sync(0xffffffffu, upto, x);
-          if (i >= end) {
-            k = x + 1;
-            before = end;
-          }
-        }
-        if (i < few) c[i] = ld_cluster64(ptx::map_to_cta(ptx::smem_u32(&sh.hist[buf][i - before]), k));
-      }
+      pull_few<NT>(c, sh.hist[buf], count, few, a.splits);
     }
     if (a.splits > 1) {
       ptx::cluster_arrive();

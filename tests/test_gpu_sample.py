@@ -260,3 +260,17 @@ def test_many_rows(dc, vocab, stride, dtype):
     check(dc, l, u, T=0.5 + 0.01 * r, k=np.where(r % 2 == 0, 0, 1 + r * vocab // 300), p=np.where(r % 4 < 2, 1.0, (r + 1) / 151))
     check(dc, l, u, p=np.full(n, 0.5), T=np.where(r % 2 == 0, 1e30, 0.7))
     check(dc, l, u, T=np.zeros(n))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [9000, 100003])
+def test_flat_rows(dc, vocab, dtype):
+    """Cuts in the middle of a broad distribution: many logits share the last bin, more than one CTA has some."""
+    rng = np.random.default_rng(vocab + 1)
+    n = 12
+    l = torch.tensor(rng.standard_normal((n, vocab)), device="cuda").to(TYPES[dtype])
+    u = rng.random(n)
+    r = np.arange(n)
+    check(dc, l, u, p=(r + 0.5) / n, T=0.3 + 0.3 * r)
+    check(dc, l, u, k=1 + r * vocab // n, T=0.3 + 0.3 * r)
+    check(dc, l, u, k=1 + r * vocab // n, p=np.full(n, 0.6), T=0.3 + 0.3 * r, m=np.full(n, 0.001))
