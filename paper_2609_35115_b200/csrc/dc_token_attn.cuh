@@ -25,10 +25,10 @@ struct ChunkArgs {
   CUtensorMap kmap, vmap;  // [sessions * kv_heads * rows][D], boxes of 64 rows x 64 values
 };
 
-template <typename T>
+template <typename T, int N>
 __device__ __forceinline__ constexpr uint32_t chunk_idesc(int b_mn_major) {
   // fp32 accumulation, operand types (0: fp16, 1: bf16), N / 8, M / 16
-  return (1u << 4) | (sizeof(T) && Num<T>::is_bf16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(CH_N >> 3) << 17) |
+  return (1u << 4) | (sizeof(T) && Num<T>::is_bf16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) |
          ((uint32_t)(CH_M >> 4) << 24);
 }
 // D[tmem] (+)= A[tmem] * B[smem]: a 32-bit column of A holds two neighbouring values of the reduction
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
     }
     __syncwarp();
   } else if (warp == 5) {                                    // ---- products
-    const uint64_t dq = ptx::umma_desc_sw128(ptx::smem_u32(sQ)), dk = ptx::umma_desc_sw128(ptx::smem_u32(sK)), dv = ptx::umma_desc_sw128(ptx::smem_u32(sV));
+    const uint64_t dq = ptx::umma_desc_sw128(ptx::smem_u32(sQ)), dk = ptx::umma_desc_sw128(ptx::smem_u32(sK)), dv = ptx::umma_desc_sw128(ptx::smem_u32(sV)) + ((uint64_t)(KVBOX / 16 - 1) << 16);   // (columns behind the 64th: the next box)
     auto scores = [&](int j) {
       const int st = j % CH_STAGES;
       if (!warp_wait(&bars.k_full[st], (j / CH_STAGES) & 1)) return false;
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
       if (ptx::elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          ptx::umma_bf16(tmem + (j & 1) * CH_N, dq + ((k / 4) * QBOX + (k % 4) * 32) / 16, dk + (st * KVTILE + (k / 4) * KVBOX + (k % 4) * 32) / 16, chunk_idesc<T>(0), k > 0);
+          ptx::umma_bf16(tmem + (j & 1) * CH_N, dq + ((k / 4) * QBOX + (k % 4) * 32) / 16, dk + (st * KVTILE + (k / 4) * KVBOX + (k % 4) * 32) / 16, chunk_idesc<T, CH_N>(0), k > 0);
         ptx::umma_commit(&bars.k_empty[st]);
         ptx::umma_commit(&bars.s_full[j & 1]);
       }
@@ -203,10 +203,8 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
       ptx::tc_fence_after();
       if (ptx::elect_one()) {
 #pragma unroll
-        for (int b = 0; b < BOXES; ++b)
-#pragma unroll
-          for (int k = 0; k < CH_N / 16; ++k)
-            umma_ts(tmem + CH_O + b * 64, tmem + (j & 1) * CH_N + k * 8, dv + (st * KVTILE + b * KVBOX + k * 2048) / 16, chunk_idesc<T>(1), j > 0 || k > 0);
+        for (int k = 0; k < CH_N / 16; ++k)
+          umma_ts(tmem + CH_O, tmem + (j & 1) * CH_N + k * 8, dv + (st * KVTILE + k * 2048) / 16, chunk_idesc<T, D>(1), j > 0 || k > 0);
         ptx::umma_commit(&bars.v_empty[st]);
         ptx::umma_commit(&bars.pv_done[j & 1]);
       }
