@@ -472,8 +472,9 @@ typedef struct dc_qk_norm {
 } dc_qk_norm;
 
 /* Opens a cache over the caller's memory, which stays the caller's and must outlive the handle.  Nothing is written to it: a session
- * begins with its first token at position 0.  Device: the current one; calls on the cache are made with it current
- * (DC_ERR_ARG otherwise).  Synchronous; dc_cache_close too. */
+ * begins with its first token at position 0.  k_dev and v_dev do not overlap.  Device: the current one; calls on the cache are made
+ * with it current (DC_ERR_ARG otherwise).  Neither call allocates device memory or waits for the device; dc_cache_close frees the handle
+ * alone, calls that are in flight may finish behind it. */
 dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void* v_dev, dc_cache** out);
 dc_status dc_cache_close(dc_cache* cache);
 

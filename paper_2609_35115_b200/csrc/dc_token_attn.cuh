@@ -16,8 +16,12 @@
 constexpr int CH_M = 128, CH_N = STEP_N, CH_STAGES = 2, CH_THREADS = 192;
 constexpr uint32_t CH_TMEM = 256, CH_O = 128;   // columns: scores at 0 and 64, output at 128
 
+// Never less than a third of an SM's: with three CTAs on an SM the third would wait for tensor memory while its cluster waits for it.
 template <int D>
-constexpr size_t chunk_smem() { return 1024 + (size_t)CH_M * D * 2 + (size_t)CH_STAGES * 2 * CH_N * D * 2; }
+constexpr size_t chunk_smem() {
+  const size_t need = 1024 + (size_t)CH_M * D * 2 + (size_t)CH_STAGES * 2 * CH_N * D * 2;
+  return need < 80 * 1024 ? 80 * 1024 : need;
+}
 
 struct ChunkArgs {
   AttendArgs  a;

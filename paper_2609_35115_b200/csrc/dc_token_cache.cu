@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <mutex>
 #include <new>
 
 #include "dc_internal.h"
@@ -588,11 +589,37 @@ bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) !
 }  // namespace
 }  // namespace dc
 
+// Words that a bounded device-side wait sets when it gives up: part of the library image, so that opening and closing a cache allocates
+// nothing on the device, waits for nothing and may happen while a stream is being captured.
+static __device__ int g_cache_err[4096];
+
+namespace {
+constexpr int kErrWords = 4096;
+bool       g_err_used[kErrWords];
+std::mutex g_err_mu;
+
+// A free word (the last one is shared by all caches behind the 4095th).
+int take_err_word() {
+  std::lock_guard<std::mutex> lk(g_err_mu);
+  for (int i = 0; i < kErrWords - 1; ++i)
+    if (!g_err_used[i]) {
+      g_err_used[i] = true;
+      return i;
+    }
+  return kErrWords - 1;
+}
+void give_err_word(int i) {
+  std::lock_guard<std::mutex> lk(g_err_mu);
+  g_err_used[i] = false;
+}
+}  // namespace
+
 struct dc_cache {
   dc::CacheDims d;
   int   head_dim, dtype, device, n_sm;
   void *k, *v;
-  int*  err;      // device word that a bounded wait sets when it gives up
+  int   err_word;
+  int*  err;      // its address
   CUtensorMap kmap, vmap;
 };
 
@@ -697,6 +724,8 @@ extern "C" dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void
   if (((double)cfg->n_sink + cfg->ring_rows) * cfg->n_kv_heads * cfg->n_sessions >= 2147483648.0)
     DC_REFUSE(DC_ERR_CONFIG, "dc_cache_open: the cache has 2^31 rows or more (sessions x key/value heads x rows)");
   if (dc::misaligned(k_dev) || dc::misaligned(v_dev)) DC_REFUSE(DC_ERR_ARG, "dc_cache_open: k_dev and v_dev must be 16-byte aligned");
+  const uintptr_t bytes = ((uintptr_t)cfg->n_sink + cfg->ring_rows) * cfg->n_kv_heads * cfg->n_sessions * cfg->head_dim * 2, kp = (uintptr_t)k_dev, vp = (uintptr_t)v_dev;
+  if (kp < vp + bytes && vp < kp + bytes) DC_REFUSE(DC_ERR_ARG, "dc_cache_open: k_dev and v_dev overlap");
   dc_cache* c = new (std::nothrow) dc_cache();
   if (!c) DC_REFUSE(DC_ERR_OOM, "dc_cache_open: out of host memory");
   c->d = dc::CacheDims{cfg->n_sessions, cfg->n_heads, cfg->n_kv_heads, cfg->n_sink, cfg->window, cfg->ring_rows};
@@ -704,7 +733,6 @@ extern "C" dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void
   c->dtype = cfg->dtype;
   c->k = k_dev;
   c->v = v_dev;
-  c->err = nullptr;
   int major = 0;
   cudaError_t e = cudaGetDevice(&c->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, c->device);
@@ -724,21 +752,22 @@ extern "C" dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void
     delete c;
     DC_REFUSE(DC_ERR_CUDA, "dc_cache_open: cuTensorMapEncodeTiled failed or is unavailable");
   }
-  if (e == cudaSuccess) e = dc::dev_alloc(&c->err, sizeof(int));
-  if (e == cudaSuccess) e = cudaMemset(c->err, 0, sizeof(int));
+  void* words = nullptr;
+  if (e == cudaSuccess) e = cudaGetSymbolAddress(&words, g_cache_err);
   if (e != cudaSuccess) {
-    dc::dev_free(c->err);
     delete c;
-    DC_REFUSE(e == cudaErrorMemoryAllocation ? DC_ERR_OOM : DC_ERR_CUDA, "dc_cache_open: %s", cudaGetErrorString(e));
+    DC_REFUSE(DC_ERR_CUDA, "dc_cache_open: %s", cudaGetErrorString(e));
   }
+  c->err_word = take_err_word();
+  c->err = static_cast<int*>(words) + c->err_word;
   *out = c;
   return DC_OK;
 }
 
 extern "C" dc_status dc_cache_close(dc_cache* c) {
   if (!c) DC_REFUSE(DC_ERR_ARG, "dc_cache_close: null pointer argument");
-  dc::dev_free(c->err);     // (waits for the device: no call of this cache is in flight behind it)
-  delete c;
+  give_err_word(c->err_word);
+  delete c;                 // (calls in flight have all they need as arguments)
   return DC_OK;
 }
 

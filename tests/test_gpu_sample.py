@@ -222,7 +222,7 @@ def test_shares_of_many_draws(dc):
     assert (got - n * torch.softmax(row.double(), 0)).abs().max() <= 1.0 + n * 2.0 ** -24      # (u is rounded to fp32)
 
 
-@pytest.mark.parametrize("T", [1e30, 1e38, 3e4, 50.0])
+@pytest.mark.parametrize("T", [np.inf, 1e30, 1e38, 3e4, 50.0])
 def test_scores_closer_than_weights_can_tell(dc, T):
     """High temperatures: neighbouring logits have equal weights, and their order still decides who is kept."""
     rng = np.random.default_rng(17)

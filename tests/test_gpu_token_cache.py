@@ -318,11 +318,6 @@ def test_refusals(dc):
 # ---- a step as it is used ------------------------------------------------------------------------------------------------------------
 
 
-def generate(dc, c, qkvs, norm, step):
-    """Tokens one by one through append and attend; step(i, qkv) runs the two and returns the outputs."""
-    return [step(qkv).clone() for qkv in qkvs]
-
-
 def test_a_prompt_and_steps_agree_with_one_long_prompt(dc):
     """A prompt, then single tokens, against the same positions as one prompt: every token sees the same rows, whatever call brought it."""
     T, n0, d, H, Hkv = 150, 61, 128, 8, 2
@@ -401,3 +396,75 @@ def test_a_cache_with_offsets_behind_32_bits(dc):
         assert ((out.double() - want).abs() <= bound).all()
         assert torch.equal(v[pool - 1][:, r[-1]], qkv.view(T, 24, d)[-1, 16:])
     cache.close()
+
+
+def test_caches_come_and_go_while_a_step_is_captured(dc):
+    """Opening, using and closing a cache inside of a capture: nothing of it touches the device outside of the stream."""
+    c = Case(dc, new=(1, 1), start=(40, 3), d=64, H=4, Hkv=2, cu=False, seed=9)
+    q = c.normal(2, 4, 64)
+    want = c.cache.attend(q, c.batch)
+    out = torch.zeros_like(q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        again = dc.TokenCache(c.k, c.v, 4, c.n_sink, c.window)
+        again.attend(q, c.batch, out=out)
+        again.close()
+        del again
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_two_graphs_over_one_cache_at_once(dc):
+    """Two captured steps of different sessions of one cache, replayed on two streams: calls have no memory of their own to share."""
+    c = Case(dc, new=(1,) * 8, start=(900,) * 8, d=128, H=8, Hkv=2, window=600, cu=False, seed=10)
+    parts = [dc.TokenBatch(i32(c.order[i:i + 4]), i32([900] * 4)) for i in (0, 4)]
+    q = [c.normal(4, 8, 128) for _ in parts]
+    want = [c.cache.attend(x, b) for x, b in zip(q, parts)]
+    torch.cuda.synchronize()
+    streams, graphs, outs = [torch.cuda.Stream() for _ in parts], [], []
+    for x, b, s in zip(q, parts, streams):
+        o, g = torch.zeros_like(x), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            for _ in range(10):
+                c.cache.attend(x, b, out=o)
+        graphs.append(g)
+        outs.append(o)
+    for _ in range(10):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_chunks_beside_the_flow_decoder(dc):
+    """A chunk's attention (tensor memory, clusters) on one stream, the flow decoder on another."""
+    import numpy as np
+    import dc_workloads as wl
+    cfg = wl.tiny_flow(name="beside", n_chunks=3, seed=3)
+    w = wl.make_workload(cfg)
+    m = dc.Model(cfg, w.weights)
+    st = m.open_stream()
+    feats = torch.from_numpy(np.ascontiguousarray(w.streams[0].feats[:cfg.f_chunk])).cuda()
+    c = Case(dc, new=(40,) * 4, start=(300,) * 4, d=64, H=16, Hkv=2, window=300, seed=11)
+    q = c.normal(c.total, 16, 64)
+    want = c.cache.attend(q, c.batch)
+    first = st.decode_chunk(feats).clone()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = [torch.empty_like(q) for _ in range(30)]
+    got = []
+    for o in outs:
+        with torch.cuda.stream(b):
+            st.reset(stream=b)
+            got.append(st.decode_chunk(feats, out=torch.empty(feats.shape[0] * m.out_per_frame, device="cuda"), stream=b))
+        c.cache.attend(q, c.batch, out=o, stream=a)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs) and all(torch.equal(x.reshape(-1), first.reshape(-1)) for x in got)
+    assert m.counters()[4] == 0
+    c.cache.check()
+    st.close()
+    m.destroy()

@@ -120,6 +120,8 @@ def test_cache_configurations_outside_of_the_kernels_are_refused(kw):
 def test_null_and_misaligned_caches_are_refused():
     assert open_raw(k=None) == "DC_ERR_ARG" and open_raw(v=None) == "DC_ERR_ARG"
     assert open_raw(k=0x10008) == "DC_ERR_ARG" and open_raw(v=0x20002) == "DC_ERR_ARG"
+    assert open_raw(v=0x10000) == "DC_ERR_ARG"                                   # one memory for both
+    assert open_raw(v=0x10000 + 2 * 2 * 44 * 64 * 2 - 16) == "DC_ERR_ARG"        # the last 16 bytes shared
     lib = dc.load_library()
     assert lib.dc_cache_open(None, 0x10000, 0x20000, None) == 1
     assert lib.dc_cache_close(None) == 1 and lib.dc_cache_check(None) == 1
