@@ -24,6 +24,7 @@ constexpr int SMP_BINS = 1024;
 constexpr int SMP_FEW = SMP_THREADS;       // candidates that one CTA finishes at most, one a thread (they lie where a histogram does)
 constexpr int SMP_SLICE = 8192;           // logits of a CTA, while 16 CTAs are enough (then up to twice as many)
 constexpr int SMP_MAX_CLUSTER = 16;
+static_assert(DC_SAMPLE_MAX_VOCAB / 2 / SMP_WIDE <= 256 && DC_SAMPLE_MAX_VOCAB / SMP_MAX_CLUSTER / SMP_THREADS <= 256, "logits of a thread: their weights are summed exactly");
 constexpr uint32_t KEY_NONE = 0x007fffffu;   // key of -infinity: such logits, and NaN, take no part
 constexpr unsigned long long ONE = 1ull << 45;
 constexpr float LOWEST = -3.402823466e38f;
@@ -781,17 +782,30 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
   // ---- the draw: running mass in the vocabulary's order ------------------------------------------------------------------------------
   unsigned long long seen = ties_before, sum = 0;
   constexpr int U = STREAM ? 4 : 2;      // steps whose loads are under way at once
+  double whole = 0.0;
   for (int i0 = warp * part + lane * 4; i0 < (warp + 1) * part; i0 += U * STEP) {
     float4 v[U];
 #pragma unroll
     for (int x = 0; x < U; ++x) v[x] = i0 + x * STEP < (warp + 1) * part ? row.quad(i0 + x * STEP) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
 #pragma unroll
     for (int x = 0; x < U; ++x) {
-      unsigned long long m[4];
-      weights(v[x], seen, m);
-      sum += (m[0] + m[1]) + (m[2] + m[3]);
+      if (cut.ties) {
+        unsigned long long m[4];
+        weights(v[x], seen, m);
+        sum += (m[0] + m[1]) + (m[2] + m[3]);
+      } else if (fmaxf(fmaxf(v[x].x, v[x].y), fmaxf(v[x].z, v[x].w)) >= cut.low) {
+        // (multiples of 2^-45 whose sum, of 256 at most, is exact in fp64: fewer integer operations)
+        const float y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+        double r[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = __dadd_rn(__dadd_rn(w.value(y[e]), 128.0), -128.0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (y[e] >= cut.low) whole += r[e];
+      }
     }
   }
+  sum += (unsigned long long)(whole * (double)ONE);
   sum = warp_sum(sum);
   __syncthreads();
   if (lane == 0) sh.warp_sum[warp] = sum;
