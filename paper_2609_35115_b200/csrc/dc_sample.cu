@@ -1,13 +1,17 @@
 // Choice of the next token from rows of logits (include/dc.h, dc_sample_tokens): temperature, top-k, top-p, min-p, from given random numbers.
 //
-// One pass over the logits: a cluster of CTAs keeps a row in shared memory, each CTA a contiguous slice of the vocabulary, and
-// everything after the load happens there.  The rules cut a prefix of the order "descending logit, ties by lowest index", so the kept set is
+// A cluster of CTAs keeps a row in shared memory, each CTA a contiguous slice of the vocabulary, and everything after the load happens
+// there; rows enough for every SM are streamed from memory instead, pass by pass, by one or two CTAs each.  The rules cut a prefix of the order "descending logit, ties by lowest index", so the kept set is
 // a cut key and a number of its ties; cuts are found by selection through histograms, by counts (top-k) or by mass (top-p).
 //
 // The result is a whole number that has to be the right one, so masses are exact: a weight exp((l - max) / T) is evaluated in fp64
 // (2^(j/256) from a table times a polynomial; about 2^-50) and held as an integer multiple of 2^-45.  Integer sums do not depend on their order: atomics, splits
 // and replays give the same token.  Against sums in real arithmetic a border is off by at most 2^-46 for every token of the row; a
 // border that close to a row's random number is met once in millions of rows.
+//
+// Bound by the latency of the passes and of the cluster's barriers between them (few rows), by the passes' instructions, fp64 and shared-memory adds
+// among them (many).  Measured, 256 rows of 131,072 fp32 logits: greedy 37 us, no rule 106 us, top-k 50 85 us, top-p 0.9 247 us; 48 rows of 32,001: 10, 12, 15, 27 us; one
+// of 4,097: 8 to 10 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>

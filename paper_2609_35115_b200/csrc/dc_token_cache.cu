@@ -87,6 +87,7 @@ constexpr int APPEND_DEPTH = 8;    // 16-byte pieces that a lane has in flight
 // A head is D / 8 neighbouring lanes of 16 bytes each, so the sum of squares and the partner of a
 // rotated pair come from shuffles, every value is read once and written once, and a lane's gains and angles are the same for
 // all heads; two values go through each operation.  The angle is position * inv_freq in 64 bits, in turns, whose fraction is exact enough in 32 for sincospi.
+// Measured: 6,162 tokens of 48 heads of 128, 28.7 us, 5.3 TB/s (43 us with four pieces a lane in registers in flight instead of eight in shared memory).
 template <typename T, int D, bool INTER>
 __global__ void __launch_bounds__(APPEND_WARPS * 32, 3) append_kernel(const AppendArgs a) {
   constexpr int LPH = D / 8;
@@ -287,7 +288,8 @@ constexpr int step_smem(int warps) { return warps * STEP_STAGES * STEP_UNIT; }
 // running maximum, sum and output in registers; no warp waits for another before the end.  The products (m16n8k16) have the rows of K, or the
 // columns of V, as their 16 rows and the query heads that share a K/V head as their 8 columns (NH = 2: twice 8): a row is read once for
 // all of them, and a group of up to 8 heads takes 8 + 16 products a unit.  (With the heads as the 16 rows it took 48, and
-// those, at about 35 cycles each, bounded the kernel: 36 us against 18 for one session of 32,768 rows.)  The units of a
+// those, at about 35 cycles each, bounded the kernel: 36 us against 20 for one session of 32,768 rows.)  Measured: 48 sessions of up to 4,100 rows, 8 x 128 values of K and of V each,
+// 98 us, 6.4 TB/s; one session of 32,768 rows, 4 heads, 20 us, 3.3 TB/s: its four clusters sit in four of the device's eight GPCs.  The units of a
 // (sequence, head) are dealt out over the warps of a cluster of CTAs, which joins the partial results through distributed shared
 // memory: no workspace, no second launch.  The numerators enter the second product as two halves (their rounding to 16 bits and what
 // that leaves), so that the result is rounded once.
@@ -799,7 +801,8 @@ extern "C" dc_status dc_cache_append(dc_cache* c, const dc_token_batch* b, const
     DC_REFUSE(DC_ERR_ARG, "%s: qkv_dev and q_dev must be 16-byte aligned, their row strides multiples of 8 values and no shorter than a row", who);
   if (q_dev == qkv_dev && q_stride != qkv_stride) DC_REFUSE(DC_ERR_ARG, "%s: queries written in place keep the rows' stride", who);
   dc::AppendArgs a{c->d, kernel_batch(b), qkv_dev, qkv_stride, q_stride, q_dev, c->k, c->v, nm->q_gain_dev, nm->k_gain_dev, nm->inv_freq_dev, nm->rot_dim, nm->eps, dc::APPEND_WARPS};
-  // A token's row is dealt out over a whole CTA's warps while that gives an SM no more than 32 warps to run, and over fewer behind that.
+  // A token's row is dealt out over a whole CTA's warps while that gives an SM no more than 32 warps to run, and over fewer behind that (6,162 tokens: 43, 33,
+  // 30 and 29 us in 8, 4, 2 and 1 warps a row; 64 tokens: 2.6 us in 8).
   while (a.share > 1 && (long long)b->n_tokens * a.share > 32ll * c->n_sm) a.share /= 2;
   const long long warps = (long long)b->n_tokens * a.share;
   return launched(dc::launch(append_fn(c->dtype, D, nm->interleaved != 0), dim3((unsigned)((warps + dc::APPEND_WARPS - 1) / dc::APPEND_WARPS)), dc::APPEND_WARPS * 32, 0, 1,
@@ -823,7 +826,8 @@ extern "C" dc_status dc_cache_attend(dc_cache* c, const dc_token_batch* b, const
     const int per = dc::CH_M / a.group;
     ca.tiles = (b->max_tokens + per - 1) / per;
     const long long tiles = (long long)ca.tiles * c->d.n_kv_heads * b->n_seqs, steps = (seen + per) / dc::CH_N + 1;
-    // Splits of a tile's rows over a cluster: while all CTAs are resident (two per SM) and each has two steps or more.
+    // Splits of a tile's rows over a cluster: while all CTAs are resident (two per SM) and each has two steps or more (chunks of 50 tokens, 8 sessions, 13 steps
+    // of 64 rows: 21, 19, 18 and 25 us in 1, 2, 4 and 8).
     while (ca.a.splits < 16 && tiles * ca.a.splits * 2 <= 2ll * c->n_sm && ca.a.splits * 4 <= steps) ca.a.splits *= 2;
     if ((long long)ca.tiles * ca.a.splits > INT_MAX) DC_REFUSE(DC_ERR_ARG, "%s: too many tokens", who);
     return launched(dc::launch(chunk_fn(c->dtype, D), dim3(ca.tiles * ca.a.splits, c->d.n_kv_heads, b->n_seqs), dc::CH_THREADS, chunk_smem_bytes(D), ca.a.splits,
@@ -833,9 +837,10 @@ extern "C" dc_status dc_cache_attend(dc_cache* c, const dc_token_batch* b, const
   const int per = two ? 16 : 8, groups = (a.group + per - 1) / per;
   const long long units = seen * D * 2 / dc::STEP_HALF + 1, pairs = (long long)b->n_seqs * c->d.n_kv_heads * groups;
   // Splits: while every warp has a unit of its own, and either the CTAs are resident (two per SM) or, of many long rows, up to four
-  // for the balance of the last wave (48 sessions x 8 heads of 4,100 rows: 126 us unsplit, 115 us in two or four, 148 us in eight).
+  // for the balance of the last wave (48 sessions x 8 heads of up to 4,100 rows: 112 us unsplit, 104 us in two, 98 us in four, 133 us in eight).
   while (a.splits < 16 && a.splits * 2 * 4 <= units && (pairs * a.splits * 2 <= 2ll * c->n_sm || (a.splits < 4 && units >= 64 * a.splits))) a.splits *= 2;
-  // CTAs of 8 warps, one per SM, where there are fewer CTAs than SMs and rows enough: the copies in flight on an SM are what bounds it then.
+  // CTAs of 8 warps, one per SM, where there are fewer CTAs than SMs and rows enough: the copies in flight on an SM are what bounds it then (one session
+  // of 32,768 rows: 20 us against 25 us in CTAs of 4).
   const bool wide = pairs * a.splits <= c->n_sm && (long long)a.splits * 8 * 2 <= units;
   return launched(dc::launch(step_fn(c->dtype, D, two, wide), dim3(a.splits, c->d.n_kv_heads * groups, b->n_seqs), wide ? 256 : 128, dc::step_smem(wide ? 8 : 4), a.splits,
                              (cudaStream_t)cuda_stream, &a), who);
