@@ -493,7 +493,7 @@ dc_status dc_cache_append(dc_cache* cache, const dc_token_batch* batch, const dc
 /* Attention of the batch's tokens, whose own keys and values have been appended, over their sessions' rows:
  * out = sum_p w_p v_p / sum_p w_p with w_p = exp(scale * <q, k_p>) over the positions p that the token sees; query head h
  * reads key/value head h / (n_heads / n_kv_heads).  Scores, sums and outputs are held in fp32 until the one rounding of the result; in
- * calls of several tokens the numerators are rounded to the cache's type before the product with v.  scale > 0.
+ * calls of several tokens the numerators are rounded to the cache's type before the product with v.  0 < scale <= 1e30.
  *   q_dev, out_dev : [n_tokens] rows of n_heads * head_dim values, q_stride / out_stride values apart (multiples of 8).  No overlap with
  *                    each other or with the cache. */
 dc_status dc_cache_attend(dc_cache* cache, const dc_token_batch* batch, const void* q_dev, long long q_stride, float scale,

@@ -428,21 +428,25 @@ def _vector(name, t, dtype, n=None, index=None):
     """Checks a small device array that a call reads or writes; returns its address (None: none)."""
     if t is None:
         return None
-    if t.dtype is dtype and t.dim() == 1 and t.is_contiguous() and t.get_device() == (t.get_device() if index is None else index) and t.is_cuda and (n is None or t.numel() == n):
+    at = t.get_device()      # (-1: not on a CUDA device)
+    if t.dtype is dtype and at >= 0 and (index is None or at == index) and t.dim() == 1 and t.is_contiguous() and (n is None or t.numel() == n):
         return t.data_ptr()
     raise ValueError(f"{name}: a contiguous vector of {'' if n is None else f'{n} '}{dtype} on the call's CUDA device is wanted, not {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
 class TokenBatch:
     """dc_token_batch: the sequences of a call.  start (and sessions, cu_tokens) are CUDA int32 vectors that the program may rewrite in
-    place between calls or graph replays; the object keeps references to them."""
+    place between calls or graph replays; the object keeps references to them.  With cu_tokens, n_tokens is the number of rows of the call's
+    matrices and max_tokens the most that one sequence brings (a sequence that brings more is left out)."""
 
-    def __init__(self, sessions, start, cu_tokens=None, n_tokens: Optional[int] = None, max_tokens: int = 1):
+    def __init__(self, sessions, start, cu_tokens=None, n_tokens: Optional[int] = None, max_tokens: Optional[int] = None):
         import torch
+        if cu_tokens is not None and (n_tokens is None or max_tokens is None):
+            raise ValueError("n_tokens and max_tokens are needed with cu_tokens")
         self.index, n = start.get_device(), start.shape[0]
         self._kept = (sessions, start, cu_tokens)
         self.c = c = dc_token_batch()
-        c.size, c.n_seqs, c.max_tokens = C.sizeof(dc_token_batch), n, max_tokens
+        c.size, c.n_seqs, c.max_tokens = C.sizeof(dc_token_batch), n, 1 if max_tokens is None else max_tokens
         c.n_tokens = n if n_tokens is None else n_tokens
         c.start_dev = _vector("start", start, torch.int32, n)
         c.sessions_dev = _vector("sessions", sessions, torch.int32, n, self.index)

@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   }
   if (!ok) {
     bars.failed = 1;
-    *a.err = 1;
+    *a.err = a.err_id;
   }
   __syncthreads();                                           // every product of this CTA has completed, or a wait has given up
   const bool failed = bars.failed != 0;

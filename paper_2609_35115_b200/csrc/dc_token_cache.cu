@@ -237,7 +237,8 @@ struct AttendArgs {
   float       scale_log2e;
   int         group;     // query heads of a key/value head
   int         splits;    // CTAs of a cluster
-  int*        err;
+  int*        err;       // where a bounded wait that gives up writes err_id
+  int         err_id;
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
@@ -601,8 +602,10 @@ bool       g_err_used[kErrWords];
 std::mutex g_err_mu;
 
 // A free word (the last one is shared by all caches behind the 4095th).
-int take_err_word() {
+int take_err_word(int* id) {
+  static int opened = 0;
   std::lock_guard<std::mutex> lk(g_err_mu);
+  *id = opened = opened == INT_MAX ? 1 : opened + 1;
   for (int i = 0; i < kErrWords - 1; ++i)
     if (!g_err_used[i]) {
       g_err_used[i] = true;
@@ -620,8 +623,8 @@ struct dc_cache {
   dc::CacheDims d;
   int   head_dim, dtype, device, n_sm;
   void *k, *v;
-  int   err_word;
-  int*  err;      // its address
+  int   err_word, err_id;   // this cache's number: what another one has left in the word is not taken for its own
+  int*  err;                // the word's address
   CUtensorMap kmap, vmap;
 };
 
@@ -760,7 +763,7 @@ extern "C" dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void
     delete c;
     DC_REFUSE(DC_ERR_CUDA, "dc_cache_open: %s", cudaGetErrorString(e));
   }
-  c->err_word = take_err_word();
+  c->err_word = take_err_word(&c->err_id);
   c->err = static_cast<int*>(words) + c->err_word;
   *out = c;
   return DC_OK;
@@ -775,12 +778,14 @@ extern "C" dc_status dc_cache_close(dc_cache* c) {
 
 extern "C" dc_status dc_cache_check(dc_cache* c) {
   if (!c) DC_REFUSE(DC_ERR_ARG, "dc_cache_check: null pointer argument");
-  int word = 0;
-  cudaError_t e = cudaDeviceSynchronize();
+  int word = 0, dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && dev != c->device) DC_REFUSE(DC_ERR_ARG, "dc_cache_check: the cache is on device %d, the current device is %d", c->device, dev);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = cudaMemcpy(&word, c->err, sizeof(int), cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess && word) e = cudaMemset(c->err, 0, sizeof(int));
+  if (e == cudaSuccess && word == c->err_id) e = cudaMemset(c->err, 0, sizeof(int));
   if (e != cudaSuccess) DC_REFUSE(DC_ERR_CUDA, "dc_cache_check: %s", cudaGetErrorString(e));
-  if (word) DC_REFUSE(DC_ERR_TIMEOUT, "dc_cache_check: a bounded device-side wait of an attention call gave up; its outputs are not valid");
+  if (word == c->err_id) DC_REFUSE(DC_ERR_TIMEOUT, "dc_cache_check: a bounded device-side wait of an attention call gave up; its outputs are not valid");
   return DC_OK;
 }
 
@@ -814,12 +819,12 @@ extern "C" dc_status dc_cache_attend(dc_cache* c, const dc_token_batch* b, const
   const char* who = "dc_cache_attend";
   dc_status st = admit_batch(c, b, who);
   if (st != DC_OK) return st;
-  if (!(scale > 0.f) || isinf(scale)) DC_REFUSE(DC_ERR_ARG, "%s: scale must be positive and finite", who);
+  if (!(scale > 0.f) || scale > 1e30f) DC_REFUSE(DC_ERR_ARG, "%s: scale must be positive, 1e30 at most", who);
   const int D = c->head_dim;
   const long long width = (long long)c->d.n_heads * D;
   if (bad_rows(q_dev, q_stride, width) || bad_rows(out_dev, out_stride, width))
     DC_REFUSE(DC_ERR_ARG, "%s: q_dev and out_dev must be 16-byte aligned, their row strides multiples of 8 values and no shorter than a row", who);
-  dc::AttendArgs a{c->d, kernel_batch(b), q_dev, c->k, c->v, out_dev, q_stride, out_stride, scale * 1.4426950408889634f, c->d.n_heads / c->d.n_kv_heads, 1, c->err};
+  dc::AttendArgs a{c->d, kernel_batch(b), q_dev, c->k, c->v, out_dev, q_stride, out_stride, scale * 1.4426950408889634f, c->d.n_heads / c->d.n_kv_heads, 1, c->err, c->err_id};
   const long long seen = (long long)c->d.n_sink + c->d.window;     // most rows that a token sees
   if (b->max_tokens > 1) {
     dc::ChunkArgs ca{a, 0, c->kmap, c->vmap};

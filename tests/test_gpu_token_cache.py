@@ -244,6 +244,17 @@ def test_an_odd_value_reaches_the_tokens_that_see_it_and_no_other(dc, case, valu
     c.cache.check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_sink,ring,T", [(0, 1, 1), (1, 1, 1), (0, 2, 2), (2, 3, 3), (0, 63, 40), (5, 59, 59)])
+def test_the_smallest_caches(dc, n_sink, ring, T, d):
+    """Fewer rows than a box of the copies, a window that is as long as the ring lets it."""
+    c = Case(dc, new=(T,), start=(7 * ring,), d=d, H=3, Hkv=1, n_sink=n_sink, window=ring - T + 1, ring=ring, pool=1, seed=ring)
+    q = c.normal(c.total, 3, d)
+    out = torch.zeros_like(q)
+    c.cache.attend(q, c.batch, out=out)
+    c.check_attend(q, out, torch.zeros_like(q))
+
+
 # ---- batches that do not fit, refusals ---------------------------------------------------------------------------------------------
 
 
@@ -291,7 +302,7 @@ def test_refusals(dc):
     assert status(lambda: c.cache.attend(q[:5], dc.TokenBatch(i32([0, 1]), i32([0, 0]), None, 5, 1))) == "DC_ERR_ARG"
     assert status(lambda: c.cache.attend(q, dc.TokenBatch(i32([0, 1]), i32([0, 0]), i32([0, 3, 5]), 5, 0))) == "DC_ERR_ARG"
     assert status(lambda: c.cache.attend(q[:4], dc.TokenBatch(None, i32([0] * 4)))) == "DC_ERR_ARG"                               # 3 sessions
-    for scale in (0.0, -1.0, float("nan"), float("inf")):
+    for scale in (0.0, -1.0, float("nan"), float("inf"), 3e38):
         assert status(lambda: c.cache.attend(q, c.batch, scale=scale)) == "DC_ERR_ARG"
     wide = torch.zeros(5, 4 * 64 + 4, dtype=BF, device="cuda")
     assert status(lambda: c.cache.attend(wide[:, :256], c.batch)) == "DC_ERR_ARG"                 # rows 520 bytes apart
@@ -303,7 +314,7 @@ def test_refusals(dc):
     assert status(lambda: c.cache.append(qkv, c.batch, dc.QKNorm(torch.ones(64, device="cuda"), torch.ones(64, device="cuda"), eps=-1.0))) == "DC_ERR_ARG"
     for call in (lambda: c.cache.attend(q.half(), c.batch), lambda: c.cache.attend(q[:4], c.batch), lambda: c.cache.attend(q.cpu(), c.batch),
                  lambda: c.cache.attend(q.transpose(1, 2), c.batch), lambda: c.cache.append(q, c.batch, norm),
-                 lambda: dc.TokenBatch(i32([0, 1]), i32([0, 0]).long()), lambda: dc.TokenBatch(i32([0]), i32([0, 0])), lambda: dc.TokenBatch(None, i32([0, 0]), i32([0, 1])),
+                 lambda: dc.TokenBatch(i32([0, 1]), i32([0, 0]).long()), lambda: dc.TokenBatch(i32([0]), i32([0, 0])), lambda: dc.TokenBatch(None, i32([0, 0]), i32([0, 1]), 1, 1), lambda: dc.TokenBatch(None, i32([0, 0]), i32([0, 1, 2]), 2), lambda: dc.TokenBatch(None, i32([0, 0]), i32([0, 1, 2]), max_tokens=1),
                  lambda: dc.TokenCache(c.k[:, :, ::2], c.v[:, :, ::2], 4), lambda: dc.TokenCache(c.k, c.v[:2], 4), lambda: dc.QKNorm(torch.ones(64), torch.ones(64))):
         with pytest.raises(ValueError):
             call()
