@@ -28,6 +28,7 @@ constexpr int SMP_BINS = 1024;
 constexpr int SMP_FEW = SMP_THREADS;       // candidates that one CTA finishes at most, one a thread (they lie where a histogram does)
 constexpr int SMP_SLICE = 8192;           // logits of a CTA, while 16 CTAs are enough (then up to twice as many)
 constexpr int SMP_MAX_CLUSTER = 16;
+static_assert(2 * SMP_WIDE <= SMP_BINS, "a bin's logits and their masses lie where a histogram does");
 static_assert(DC_SAMPLE_MAX_VOCAB / 2 / SMP_WIDE <= 256 && DC_SAMPLE_MAX_VOCAB / SMP_MAX_CLUSTER / SMP_THREADS <= 256, "logits of a thread: their weights are summed exactly");
 constexpr uint32_t KEY_NONE = 0x007fffffu;   // key of -infinity: such logits, and NaN, take no part
 constexpr unsigned long long ONE = 1ull << 45;
@@ -57,7 +58,7 @@ struct SampleShared {
   float              at_least;               // by mass: the logits in it and above are no fewer
   uint32_t           warp_ties[SMP_WARPS];
   uint32_t           ties;                   // of the slice
-  uint32_t           few;                    // collected logits of the slice
+  uint32_t           few[2];                 // collected logits of the slice: candidates of the whole draw, and of a selection's last bin
   uint32_t           found;                  // key of a selection among few, and what lies above it
   unsigned long long found_above;
   int                bin;
@@ -404,7 +405,7 @@ __device__ __forceinline__ Selected select(SampleShared& sh, const Row<T, STREAM
   // the histogram that is free, as keys with inverted indices.  (By mass their number is not known, only that it is no less than at_least.)
   const bool try_few = may_few && (BY_MASS ? sh.at_least <= (float)SMP_FEW : above + sh.inside <= SMP_FEW);
   if (try_few) {
-    if (tid == 0) sh.few = 0;
+    if (tid == 0) sh.few[0] = 0;
     __syncthreads();
     row.each_quad([&](int i, const float4& v) {
       const float x[4] = {v.x, v.y, v.z, v.w};
@@ -412,41 +413,46 @@ __device__ __forceinline__ Selected select(SampleShared& sh, const Row<T, STREAM
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (x[e] >= low && (int)bins.place(x[e]) <= b0) {
-          const uint32_t at = atomicAdd(&sh.few, 1u);
+          const uint32_t at = atomicAdd(&sh.few[0], 1u);
           if (at < SMP_FEW) sh.hist[buf][at] = (unsigned long long)key_of(x[e]) << 32 | (uint32_t)~(index0 + i + e);
         }
     });
     cluster_or_block_sync(splits);
-    const uint32_t n = __reduce_add_sync(0xffffffffu, lane < splits ? ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few), lane)) : 0u);
+    const uint32_t n = __reduce_add_sync(0xffffffffu, lane < splits ? ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few[0]), lane)) : 0u);
     if (n <= SMP_FEW) {
       *few = (int)n;
       return SELECT_FEW;
     }
   }
-  clear();
-  row.each_logit([&](float x) {
-    if (!(x >= x_lo && x <= x_hi)) return;
-    const float t = bins.place(x);
-    if (x >= low && (int)t == b0) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
-  });
-  find_bin<false, NT>(sh, buf, above, known, splits);
-  buf ^= 1;
-  const int b1 = sh.bin;
+  // A bin with a logit for every thread at most is resolved as it is (by mass, no logit of it weighs less than its end allows), another one by bins of its own.
+  const bool small = BY_MASS ? (float)sh.inside * exp2f((float)(b0 + 1) * (1.f / 22.f) - 45.f) <= (float)NT : sh.inside <= NT;
+  int b1 = -1;
+  if (!small) {
+    clear();
+    row.each_logit([&](float x) {
+      if (!(x >= x_lo && x <= x_hi)) return;
+      const float t = bins.place(x);
+      if (x >= low && (int)t == b0) add_to_bin<BY_MASS>(&sh.hist[buf][Binned::inner(t, b0)], w, x);
+    });
+    find_bin<false, NT>(sh, buf, above, known, splits);
+    buf ^= 1;
+    b1 = sh.bin;
+  }
   auto in_bin = [&](float x) {
     if (!(x >= x_lo && x <= x_hi)) return false;
     const float t = bins.place(x);
-    return x >= low && (int)t == b0 && Binned::inner(t, b0) == b1;
+    return x >= low && (int)t == b0 && (b1 < 0 || Binned::inner(t, b0) == b1);
   };
   // one logit, as a rule, or equal ones, or a few: each CTA collects its own, with the bin's smallest and largest key (the latter inverted)
   uint32_t lo = 0xffffffffu, hi = 0xffffffffu;
-  if (tid == 0) sh.few = 0;
+  if (tid == 0) sh.few[1] = 0;
   __syncthreads();
   row.each_logit([&](float x) {
     if (in_bin(x)) {
       lo = min(lo, key_of(x));
       hi = min(hi, ~key_of(x));
-      const uint32_t at = atomicAdd(&sh.few, 1u);
-      if (at < SMP_FEW) sh.hist[buf][at] = key_of(x);
+      const uint32_t at = atomicAdd(&sh.few[1], 1u);
+      if (at < NT) sh.hist[buf][at] = key_of(x);
     }
   });
   lo = __reduce_min_sync(0xffffffffu, lo);
@@ -457,14 +463,14 @@ __device__ __forceinline__ Selected select(SampleShared& sh, const Row<T, STREAM
     lo = min(lo, (uint32_t)sh.warp_sum[i]);
     hi = min(hi, (uint32_t)(sh.warp_sum[i] >> 32));
   }
-  uint32_t count = sh.few, n = count;
+  uint32_t count = sh.few[1], n = count;
   if (splits > 1) {
     if (tid == 0) sh.range[BY_MASS] = (unsigned long long)hi << 32 | lo;
     cluster_or_block_sync(splits);
     count = 0;
     if (lane < splits) {
       const unsigned long long x = ld_cluster64(ptx::map_to_cta(ptx::smem_u32(&sh.range[BY_MASS]), lane));
-      count = ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few), lane));
+      count = ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few[1]), lane));
       lo = min(lo, (uint32_t)x);
       hi = min(hi, (uint32_t)(x >> 32));
     }
@@ -474,8 +480,8 @@ __device__ __forceinline__ Selected select(SampleShared& sh, const Row<T, STREAM
   }
   *key = lo;
   if (lo == ~hi) return SELECT_KEY;
-  if (n <= SMP_FEW) {      // every CTA takes them all and finds the same
-    unsigned long long *c = sh.hist[buf ^ 1], *mass = sh.hist[buf ^ 1] + SMP_FEW;
+  if (n <= NT) {      // every CTA takes them all and finds the same
+    unsigned long long *c = sh.hist[buf ^ 1], *mass = sh.hist[buf ^ 1] + NT;
     pull_few<NT>(c, sh.hist[buf], splits > 1 ? count : lane == 0 ? n : 0, (int)n, splits);
     buf ^= 1;              // (the collected ones stay as they are until the next histogram's barrier)
     __syncthreads();
@@ -652,7 +658,7 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
   if (top_p < 1.f && got != SELECT_FEW) {
     // of the mass that top-k left: the logits above the cut and the cut's ties (the bins hold all of those)
     if (too_many) too_many *= w.fixed(cut.tie);
-    const bool whole = got == SELECT_NONE;
+    const bool whole = cut.ties == 0;      // (the candidates are those from the cut up)
     got = select<true>(sh, row, w, bins, cut.ties ? cut.tie : cut.low, [&](unsigned long long total) { return share_of(total - too_many); }, a.splits, buf, whole, index0, &key, &few);
     if (got == SELECT_KEY) {
       const unsigned long long each = w.fixed(logit_of(key)), ties = (sh.target - sh.above + each - 1) / each;
@@ -664,7 +670,7 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
   if (got == SELECT_FEW) {
     unsigned long long *c = sh.hist[buf ^ 1], *sums = sh.hist[buf];      // (the first was read by everyone before the candidates' barrier; the second has the slice's own)
     if (rank == 0) {
-      const uint32_t count = lane < a.splits ? ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few), lane)) : 0;
+      const uint32_t count = lane < a.splits ? ld_cluster32(ptx::map_to_cta(ptx::smem_u32(&sh.few[0]), lane)) : 0;
       pull_few<NT>(c, sh.hist[buf], count, few, a.splits);
     }
     if (a.splits > 1) {
