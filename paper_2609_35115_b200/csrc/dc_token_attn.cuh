@@ -13,7 +13,7 @@
 // The running maximum moves only when a row's new maximum exceeds it by 8 (in powers of two): the numerators then stay below 2^8,
 // within fp16 too, and the output in tensor memory is rescaled in few of the steps.
 //
-// Measured: 8,192 tokens, 16 query heads over 4 of 128 values, window 2,048: 148 us in short bursts (814 TFLOP/s of what the masks leave), 166 us under
+// Measured: 8,192 tokens, 16 query heads over 4 of 128 values, window 2,048: 148 us in short bursts (814 TFLOP/s of what the masks leave), 164 us under
 // lasting load, where the clock falls with the power.  A step of 64 rows takes a CTA 1,650 cycles with another on its SM: the tensor core is busy for 1,280 of them.
 
 constexpr int CH_M = 128, CH_N = STEP_N, CH_STAGES = 2, CH_THREADS = 192;
