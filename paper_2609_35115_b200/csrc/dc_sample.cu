@@ -726,6 +726,7 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
         if (a.probs) a.probs[row_i] = (float)(w.value(logit_of((uint32_t)(me >> 32))) / ((double)sh.above / (double)ONE));
       }
     }
+    if (a.splits > 1) ptx::cluster_wait();      // the others read this CTA's count of candidates: its memory stays until all of them have arrived (they have, long ago)
     return;
   }
   if (least_key) {

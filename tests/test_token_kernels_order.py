@@ -1,0 +1,34 @@
+"""What the token kernels (csrc/dc_sample.cu, dc_token_attn.cuh) do in which order, read from their sources: faults of this kind are races and waits that a run
+rarely shows."""
+import os
+import re
+
+import pytest
+
+import paper_2609_35115_b200 as dc
+
+CSRC = os.path.join(os.path.dirname(dc.__file__), "csrc")
+
+
+def kernel(file, name):
+    """The body of a kernel, without comments."""
+    with open(os.path.join(CSRC, file)) as f:
+        text = re.sub(r"//[^\n]*", "", f.read())
+    at = re.search(r"__global__[^;{]*\b%s\(" % name, text).end()
+    at = text.index("{", at)
+    depth = 0
+    for i in range(at, len(text)):
+        depth += {"{": 1, "}": -1}.get(text[i], 0)
+        if depth == 0:
+            return text[at:i + 1]
+    raise AssertionError(name)
+
+
+def test_no_cta_of_a_sampling_cluster_leaves_while_another_may_read_its_memory():
+    """Every way out of the kernel ends at a cluster barrier that is passed, not only arrived at."""
+    body = kernel("dc_sample.cu", "sample_kernel")
+    passed = r"(?:if \(a\.splits > 1\) )?(?:cluster_or_block_sync\(a\.splits\)|ptx::cluster_wait\(\));\s*"
+    ways = [m.start() for m in re.finditer(r"\n\s*return;", body)] + [len(body) - 1]
+    assert len(ways) == 4
+    for end in ways:
+        assert re.search(passed + r"$", body[:end].rstrip() + "\n"), body[max(0, end - 300):end]
