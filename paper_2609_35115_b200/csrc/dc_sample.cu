@@ -29,7 +29,6 @@ constexpr int SMP_FEW = SMP_THREADS;       // candidates that one CTA finishes a
 constexpr int SMP_SLICE = 8192;           // logits of a CTA, while 16 CTAs are enough (then up to twice as many)
 constexpr int SMP_MAX_CLUSTER = 16;
 static_assert(2 * SMP_WIDE <= SMP_BINS, "a bin's logits and their masses lie where a histogram does");
-static_assert(DC_SAMPLE_MAX_VOCAB / 2 / SMP_WIDE <= 256 && DC_SAMPLE_MAX_VOCAB / SMP_MAX_CLUSTER / SMP_THREADS <= 256, "logits of a thread: their weights are summed exactly");
 constexpr uint32_t KEY_NONE = 0x007fffffu;   // key of -infinity: such logits, and NaN, take no part
 constexpr unsigned long long ONE = 1ull << 45;
 constexpr float LOWEST = -3.402823466e38f;
@@ -805,7 +804,7 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
         weights(v[x], seen, m);
         sum += (m[0] + m[1]) + (m[2] + m[3]);
       } else if (fmaxf(fmaxf(v[x].x, v[x].y), fmaxf(v[x].z, v[x].w)) >= cut.low) {
-        // (multiples of 2^-45 whose sum, of 256 at most, is exact in fp64: fewer integer operations)
+        // (multiples of 2^-45, whose sum is exact in fp64 up to 256: fewer integer operations)
         const float y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
         double r[4];
 #pragma unroll
@@ -814,6 +813,10 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
         for (int e = 0; e < 4; ++e)
           if (y[e] >= cut.low) whole += r[e];
       }
+    }
+    if (whole >= 128.0) {      // (4 U more weights stay far below 256)
+      sum += (unsigned long long)(whole * (double)ONE);
+      whole = 0.0;
     }
   }
   sum += (unsigned long long)(whole * (double)ONE);
