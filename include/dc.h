@@ -510,7 +510,8 @@ dc_status dc_cache_attend(dc_cache* cache, const dc_token_batch* batch, const vo
  * exact multiples of 2^-45 of the largest weight: the result depends on nothing but the row.
  *   logits_dev : [n_rows] rows of vocab logits (DC_F32, DC_BF16 or DC_F16), row_stride >= vocab values apart, 16-byte aligned (the rows behind the
  *                first need not be); u_dev: [n_rows], uniform in [0, 1) - the caller's random numbers
- *   tokens_dev : [n_rows]; probs_dev: [n_rows] or NULL: the token's share of the kept mass */
+ *   tokens_dev : [n_rows]; probs_dev: [n_rows] or NULL: the token's share of the kept mass
+ * Device: the current one, which is that of all pointers and of the stream. */
 #define DC_SAMPLE_MAX_VOCAB 262144
 typedef struct dc_sample_rules {
   uint32_t       size;           /* sizeof(dc_sample_rules)                                      */

@@ -552,12 +552,14 @@ class TokenCache:
 def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, probs=None, stream=None):
     """dc_sample_tokens: the next token of every row of logits [rows, vocab] (float32, bfloat16 or float16, rows any stride apart) from the random numbers
     u [rows] in [0, 1).  The rules are CUDA vectors [rows] (float32; top_k int32) or None: off.  Returns the tokens (int32 [rows], in `tokens` if given);
-    probs, if given, receives each token's share of the kept mass."""
+    probs, if given, receives each token's share of the kept mass.  The logits' device has to be the current one."""
     import torch
     if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError(f"logits: CUDA rows [rows, vocab] are wanted, not {tuple(logits.shape)}")
     n, vocab = logits.shape
     f32, i32, at, stride = torch.float32, torch.int32, logits.get_device(), logits.stride(0)
+    if torch.cuda.current_device() != at:      # (the library launches on the current device)
+        raise ValueError(f"logits: they are on device {at}, the current device is {torch.cuda.current_device()}")
     if tokens is None:
         tokens = torch.empty(n, dtype=i32, device=logits.device)
     r = dc_sample_rules(_RULES_SIZE, _vector("temperature", temperature, f32, n, at), _vector("top_k", top_k, i32, n, at), _vector("top_p", top_p, f32, n, at),
