@@ -121,7 +121,6 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   uint8_t* smem = smem_raw + ((1024 - (ptx::smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t *sQ = smem, *sK = sQ + BOXES * QBOX, *sV = sK + CH_STAGES * KVTILE;
   ptx::pdl_wait();
-  ptx::pdl_launch();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x % a.splits, tile = args.tiles - 1 - blockIdx.x / a.splits;   // late tokens see most rows: first
   const int kvh = blockIdx.y, G = a.group, per = CH_M / G;
@@ -156,6 +155,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = bars.tmem;
+  ptx::pdl_launch();      // behind the allocation: a dependent that takes tensor memory before its own wait must not hold what this grid waits for
 
   const T* Kg = static_cast<const T*>(a.k) + (long long)plane * D;
   const T* Vg = static_cast<const T*>(a.v) + (long long)plane * D;

@@ -32,3 +32,11 @@ def test_no_cta_of_a_sampling_cluster_leaves_while_another_may_read_its_memory()
     assert len(ways) == 4
     for end in ways:
         assert re.search(passed + r"$", body[:end].rstrip() + "\n"), body[max(0, end - 300):end]
+
+
+@pytest.mark.parametrize("file,name", [("dc_token_attn.cuh", "attend_chunk_kernel"), ("dc_flow.cu", "flow_gemm_kernel"), ("dc_flow.cu", "flow_attn_kernel")])
+def test_dependents_start_behind_the_allocation_of_tensor_memory(file, name):
+    """A dependent grid may allocate before it waits for this one: it must not find columns that a CTA of this one has yet to take."""
+    body = re.sub(r"if \(p\.empty\) \{[^}]*\}", "", kernel(file, name))      # (the form that does nothing)
+    allocated = max(m.start() for m in re.finditer(r"tmem_alloc(_pair)?\(", body))
+    assert body.count("pdl_launch") == 1 and allocated < body.index("__syncthreads();", allocated) < body.index("pdl_launch")
