@@ -327,67 +327,90 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   __syncthreads();                                           // every product of this CTA has completed, or a wait has given up
   const bool failed = bars.failed != 0;
   if (failed) ptx::pause_for_copies();
-  if (a.splits > 1) {      // every CTA of the cluster is through with its K and V: the parts go there
-    ptx::cluster_arrive();
-    ptx::cluster_wait();
-  }
   // Split tiles: CTA k finishes `own` rows from k * own on, and the others write their parts of those straight into its memory, [CTA][own][D] with the
   // 16-byte pieces of a row in the order piece ^ (row & 15).  (Writes are posted; reading the parts from the other CTAs took 8,000 cycles of a full tile, a
   // thousand a round.)
   const int own = (n_rows + a.splits - 1) / a.splits;
-  const uint32_t part_s = ptx::smem_u32(sK);
-  if (warp < 4 && !failed) {
-    const uint32_t lane_base = tmem + ((uint32_t)warp << 21);
-    T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + (live ? tl : 0)) * a.out_stride + (long long)(kvh * G + (live ? hh : 0)) * D;
-    const int to = live ? threadIdx.x / own : 0, slot = rank * own + (live ? threadIdx.x % own : 0);
-    const uint32_t part = a.splits > 1 ? ptx::map_to_cta(part_s + slot * D * 4, to) : 0;
-    auto emit = [&](int c, const float* o) {                           // 16 columns
-      if (!live) return;
-      if (a.splits == 1) {
+  const uint32_t part_s = ptx::smem_u32(sK), lane_base = tmem + ((uint32_t)warp << 21);
+  const bool whole = warp < 4 && !failed && n > 0 && !bars.odd;      // this warp's rows are in tensor memory
+  // the rows of a tile whose output is not there: none of this CTA's share is seen, or the odd ones
+  auto apart = [&](auto emit) {
+    float o[16] = {};
+    if (n == 0) {
+      for (int c = 0; c < D; c += 16) emit(c, o);
+      return;
+    }
+    const T* q = Qg + (long long)(live ? tl : 0) * a.q_stride + (live ? hh : 0) * D;
+#pragma unroll 1
+    for (int c = 0; c < D; c += 16) {
+      plain_row<T, D>(a, q, Kg, Vg, mine, steps, n, m, c, o, c == 0 ? &m_odd : nullptr, &l_odd);
+      if (c == 0) {
+        m = m_odd;
+        l = l_odd;
+      }
+      emit(c, o);
+    }
+  };
+  if (a.splits == 1) {
+    if (warp < 4 && !failed) {
+      T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + (live ? tl : 0)) * a.out_stride + (long long)(kvh * G + (live ? hh : 0)) * D;
+      auto emit = [&](int c, const float* o) {                           // 16 columns
+        if (!live) return;
         const float inv = 1.0f / l;
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = Num<T>::pack(o[2 * i] * inv, o[2 * i + 1] * inv);
         *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
         *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-      } else {
+      };
+      if (whole) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) st_cluster4(part + (((c / 4 + i) ^ (slot & 15)) << 4), o + 4 * i);
-      }
-    };
-    if (n == 0) {
-      const float o[16] = {};
-      for (int c = 0; c < D; c += 16) emit(c, o);
-    } else if (bars.odd) {
-      const T* q = Qg + (long long)(live ? tl : 0) * a.q_stride + (live ? hh : 0) * D;
-      float o[16];
-#pragma unroll 1
-      for (int c = 0; c < D; c += 16) {
-        plain_row<T, D>(a, q, Kg, Vg, mine, steps, n, m, c, o, c == 0 ? &m_odd : nullptr, &l_odd);
-        if (c == 0) {
-          m = m_odd;
-          l = l_odd;
+        for (int c = 0; c < D; c += 64) {
+          float o[64];
+          ptx::tmem_ld64(lane_base + CH_O + c, o);
+#pragma unroll
+          for (int i = 0; i < 64; i += 16) emit(c + i, o + i);
         }
-        emit(c, o);
-      }
-    } else {
-#pragma unroll
-      for (int c = 0; c < D; c += 64) {
-        float o[64];
-        ptx::tmem_ld64(lane_base + CH_O + c, o);
-#pragma unroll
-        for (int i = 0; i < 64; i += 16) emit(c + i, o + i);
+      } else {
+        apart(emit);
       }
     }
-    if (a.splits > 1 && live) {
-      st_cluster(ptx::map_to_cta(ptx::smem_u32(&bars.m[slot]), to), m);
-      st_cluster(ptx::map_to_cta(ptx::smem_u32(&bars.l[slot]), to), l);
-    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 5) ptx::tmem_dealloc(tmem, CH_TMEM);
+    return;
+  }
+  // The output leaves tensor memory, and tensor memory is given back, before this CTA waits for the others of its cluster: one of those may
+  // be waiting for columns that another kernel's CTA holds, which in turn may wait for these.
+  float o_all[D];
+  if (whole) {
+#pragma unroll
+    for (int c = 0; c < D; c += 64) ptx::tmem_ld64(lane_base + CH_O + c, o_all + c);
   }
   ptx::tc_fence_before();
   __syncthreads();
   if (warp == 5) ptx::tmem_dealloc(tmem, CH_TMEM);
-  if (a.splits == 1) return;
+  ptx::cluster_arrive();      // every CTA of the cluster is through with its K and V: the parts go there
+  ptx::cluster_wait();
+  if (warp < 4 && !failed) {
+    const int to = live ? threadIdx.x / own : 0, slot = rank * own + (live ? threadIdx.x % own : 0);
+    const uint32_t part = ptx::map_to_cta(part_s + slot * D * 4, to);
+    auto emit = [&](int c, const float* o) {
+      if (!live) return;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st_cluster4(part + (((c / 4 + i) ^ (slot & 15)) << 4), o + 4 * i);
+    };
+    if (whole) {
+#pragma unroll
+      for (int c = 0; c < D; c += 16) emit(c, o_all + c);
+    } else {
+      apart(emit);
+    }
+    if (live) {
+      st_cluster(ptx::map_to_cta(ptx::smem_u32(&bars.m[slot]), to), m);
+      st_cluster(ptx::map_to_cta(ptx::smem_u32(&bars.l[slot]), to), l);
+    }
+  }
   ptx::cluster_arrive();
   ptx::cluster_wait();      // (nobody reads or writes another CTA's memory behind this)
   const int r0 = rank * own, mine_n = min(own, n_rows - r0);

@@ -40,3 +40,10 @@ def test_dependents_start_behind_the_allocation_of_tensor_memory(file, name):
     body = re.sub(r"if \(p\.empty\) \{[^}]*\}", "", kernel(file, name))      # (the form that does nothing)
     allocated = max(m.start() for m in re.finditer(r"tmem_alloc(_pair)?\(", body))
     assert body.count("pdl_launch") == 1 and allocated < body.index("__syncthreads();", allocated) < body.index("pdl_launch")
+
+
+def test_tensor_memory_is_given_back_before_a_cta_waits_for_its_cluster():
+    """A CTA of the cluster may be waiting for columns that another kernel's CTA pair holds, and the pair for this CTA's."""
+    body = kernel("dc_token_attn.cuh", "attend_chunk_kernel")
+    assert body.rindex("tmem_dealloc") < body.index("cluster_arrive") < body.index("cluster_wait")
+    assert body.rindex("tmem_ld64(lane_base + CH_O") < body.index("cluster_arrive")
