@@ -112,8 +112,10 @@ __device__ __noinline__ void plain_row(const AttendArgs& a, const T* q, const T*
   }
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __grid_constant__ ChunkArgs args) {
+// SPLIT: a tile is shared by a cluster of a.splits CTAs, a kernel of its own for the registers that its way out takes.  (The bound of 3 caps the other form's at
+// 96: a prompt of 8,192 tokens takes 145 us in short bursts, 151 without it; two CTAs of either fit on an SM.)
+template <typename T, int D, bool SPLIT>
+__global__ void __launch_bounds__(CH_THREADS, SPLIT ? 2 : 3) attend_chunk_kernel(const __grid_constant__ ChunkArgs args) {
   constexpr int BOXES = D / 64, QBOX = CH_M * 128, KVBOX = CH_N * 128, KVTILE = BOXES * KVBOX;
   extern __shared__ uint8_t smem_raw[];
   __shared__ ChunkBars bars;
@@ -122,7 +124,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   uint8_t *sQ = smem, *sK = sQ + BOXES * QBOX, *sV = sK + CH_STAGES * KVTILE;
   ptx::pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = blockIdx.x % a.splits, tile = args.tiles - 1 - blockIdx.x / a.splits;   // late tokens see most rows: first
+  const int splits = SPLIT ? a.splits : 1, rank = blockIdx.x % splits, tile = args.tiles - 1 - blockIdx.x / splits;   // late tokens see most rows: first
   const int kvh = blockIdx.y, G = a.group, per = CH_M / G;
   const TokenSeq s = load_seq(a.b, a.d, blockIdx.z);
   const int tok0 = tile * per;
@@ -132,7 +134,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   const int plane = (s.session * a.d.n_kv_heads + kvh) * rows;     // (the cache has fewer than 2^31 rows)
   const RowSet any = seen_by_any(a.d, q_lo, q_hi), all = seen_by_all(a.d, q_lo, q_hi);
   StepList steps;
-  const int n = steps.build(any, n_sink, rank, a.splits);
+  const int n = steps.build(any, n_sink, rank, splits);
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < CH_STAGES; ++i) {
@@ -330,7 +332,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   // Split tiles: CTA k finishes `own` rows from k * own on, and the others write their parts of those straight into its memory, [CTA][own][D] with the
   // 16-byte pieces of a row in the order piece ^ (row & 15).  (Writes are posted; reading the parts from the other CTAs took 8,000 cycles of a full tile, a
   // thousand a round.)
-  const int own = (n_rows + a.splits - 1) / a.splits;
+  const int own = (n_rows + splits - 1) / splits;
   const uint32_t part_s = ptx::smem_u32(sK), lane_base = tmem + ((uint32_t)warp << 21);
   const bool whole = warp < 4 && !failed && n > 0 && !bars.odd;      // this warp's rows are in tensor memory
   // the rows of a tile whose output is not there: none of this CTA's share is seen, or the odd ones
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
       emit(c, o);
     }
   };
-  if (a.splits == 1) {
+  if constexpr (!SPLIT) {
     if (warp < 4 && !failed) {
       T* out = static_cast<T*>(a.out) + (long long)(s.first + tok0 + (live ? tl : 0)) * a.out_stride + (long long)(kvh * G + (live ? hh : 0)) * D;
       auto emit = [&](int c, const float* o) {                           // 16 columns
@@ -418,11 +420,11 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
   if ((int)threadIdx.x < mine_n) {
     const int r = threadIdx.x;
     float M = -INFINITY, L = 0.f;
-    for (int k = 0; k < a.splits; ++k) M = fmaxf(M, bars.m[k * own + r]);
+    for (int k = 0; k < splits; ++k) M = fmaxf(M, bars.m[k * own + r]);
     const float base = M == -INFINITY ? 0.f : M;
-    for (int k = 0; k < a.splits; ++k) L = fmaf(ex2(bars.m[k * own + r] - base), bars.l[k * own + r], L);
+    for (int k = 0; k < splits; ++k) L = fmaf(ex2(bars.m[k * own + r] - base), bars.l[k * own + r], L);
     const float inv = 1.0f / L;
-    for (int k = 0; k < a.splits; ++k) weight[k * own + r] = ex2(bars.m[k * own + r] - base) * inv;
+    for (int k = 0; k < splits; ++k) weight[k * own + r] = ex2(bars.m[k * own + r] - base) * inv;
   }
   __syncthreads();
   const float* parts = reinterpret_cast<const float*>(sK);
@@ -434,7 +436,7 @@ __global__ void __launch_bounds__(CH_THREADS, 2) attend_chunk_kernel(const __gri
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     int slot = r;
 #pragma unroll 2
-    for (int k = 0; k < a.splits; ++k, slot += own) {
+    for (int k = 0; k < splits; ++k, slot += own) {
       const float f = weight[slot];
       const float4 v = *reinterpret_cast<const float4*>(parts + slot * D + ((c ^ (slot & 15)) << 2));
       o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));

@@ -692,10 +692,12 @@ StepFn step_fn(int dtype, int D, bool two, bool wide) {
 }
 
 using ChunkFn = void (*)(const dc::ChunkArgs);
-ChunkFn chunk_fn(int dtype, int D) {
-  using namespace dc;
-  if (dtype == DC_BF16) return D == 128 ? attend_chunk_kernel<bf16, 128> : attend_chunk_kernel<bf16, 64>;
-  return D == 128 ? attend_chunk_kernel<__half, 128> : attend_chunk_kernel<__half, 64>;
+template <typename T, int D>
+ChunkFn chunk_of(bool split) { return split ? dc::attend_chunk_kernel<T, D, true> : dc::attend_chunk_kernel<T, D, false>; }
+// split: tiles that a cluster of CTAs shares
+ChunkFn chunk_fn(int dtype, int D, bool split) {
+  if (dtype == DC_BF16) return D == 128 ? chunk_of<dc::bf16, 128>(split) : chunk_of<dc::bf16, 64>(split);
+  return D == 128 ? chunk_of<__half, 128>(split) : chunk_of<__half, 64>(split);
 }
 size_t chunk_smem_bytes(int D) { return D == 128 ? dc::chunk_smem<128>() : dc::chunk_smem<64>(); }
 
@@ -751,8 +753,9 @@ extern "C" dc_status dc_cache_open(const dc_cache_config* cfg, void* k_dev, void
     if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim, two, wide), cudaFuncAttributeMaxDynamicSharedMemorySize, dc::step_smem(wide ? 8 : 4));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(step_fn(c->dtype, c->head_dim, two, wide), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   }
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)chunk_smem_bytes(c->head_dim));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  for (int split = 0; split < 2; ++split)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim, split), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)chunk_smem_bytes(c->head_dim));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(chunk_fn(c->dtype, c->head_dim, true), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess && !(cache_map(&c->kmap, c, k_dev) && cache_map(&c->vmap, c, v_dev))) {
     delete c;
     DC_REFUSE(DC_ERR_CUDA, "dc_cache_open: cuTensorMapEncodeTiled failed or is unavailable");
@@ -835,7 +838,7 @@ extern "C" dc_status dc_cache_attend(dc_cache* c, const dc_token_batch* b, const
     // of 64 rows: 21, 19, 18 and 25 us in 1, 2, 4 and 8).
     while (ca.a.splits < 16 && tiles * ca.a.splits * 2 <= 2ll * c->n_sm && ca.a.splits * 4 <= steps) ca.a.splits *= 2;
     if ((long long)ca.tiles * ca.a.splits > INT_MAX) DC_REFUSE(DC_ERR_ARG, "%s: too many tokens", who);
-    return launched(dc::launch(chunk_fn(c->dtype, D), dim3(ca.tiles * ca.a.splits, c->d.n_kv_heads, b->n_seqs), dc::CH_THREADS, chunk_smem_bytes(D), ca.a.splits,
+    return launched(dc::launch(chunk_fn(c->dtype, D, ca.a.splits > 1), dim3(ca.tiles * ca.a.splits, c->d.n_kv_heads, b->n_seqs), dc::CH_THREADS, chunk_smem_bytes(D), ca.a.splits,
                                (cudaStream_t)cuda_stream, &ca), who);
   }
   const bool two = a.group > 8;
