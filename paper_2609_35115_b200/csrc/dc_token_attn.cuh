@@ -61,18 +61,22 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, float v) { asm volatil
 constexpr uint32_t CH_POLLS = 1u << 18;
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait_limit(bar, parity, CH_POLLS)); }
 
+// x * scale - m takes one rounding, and so leaves what the rounding of m, itself such a product, has lost: half a step of it, a common factor of a row's numerators.
+// Up to here (2^24) that is 2^0.5 at most; far beyond it the factor leaves the types' range.
+constexpr float CH_FAR = 16777216.f;
+
 struct ChunkBars {
   uint64_t k_full[CH_STAGES], k_empty[CH_STAGES], v_full[CH_STAGES], v_empty[CH_STAGES];
   uint64_t s_full[2], p_full[2], q_full;
   uint64_t pv_done[2];   // of even and odd steps: a row's thread may see step j - 1's product done before it has looked for step j - 2's
   uint32_t tmem;
   int      failed;    // a bounded wait gave up
-  int      odd;       // a row of V that some of the tile's queries see and others do not holds an infinity or a NaN
+  int      odd;       // a row of V that some of the tile's queries see and others do not holds an infinity or a NaN, or a maximum lies beyond CH_FAR
   float    m[CH_M], l[CH_M];
 };
 
-// One query row with plain arithmetic over the steps' rows: o[0..16) of its columns c0.. .  Only for tiles with odd rows (see ChunkBars),
-// where a weight of zero may not meet a value: here masked rows are not read at all.
+// One query row with plain arithmetic over the steps' rows: o[0..16) of its columns c0.. .  Only for odd tiles (see ChunkBars):
+// masked rows, whose weight of zero may not meet a value, are not read at all, and a score is rounded before the maximum is taken off.
 template <typename T, int D>
 __device__ __noinline__ void plain_row(const AttendArgs& a, const T* q, const T* K, const T* V, const RowSet& mine, const StepList& steps, int n, float m, int c0, float* o,
                                        float* m_out, float* l_out) {
@@ -282,7 +286,10 @@ __global__ void __launch_bounds__(CH_THREADS, SPLIT ? 2 : 3) attend_chunk_kernel
       const bool move = top > m + 8.f;                       // (m = -inf: at the first row that is seen)
       if (__any_sync(0xffffffffu, move)) {
         const float f = move ? ex2(m - top) : 1.f;
-        if (move) m = top;
+        if (move) {
+          m = top;
+          if (fabsf(top) > CH_FAR && top < INFINITY) bars.odd = 1;
+        }
         l *= f;
         if (j > 0) {
           ok = warp_wait(&bars.pv_done[(j - 1) & 1], ((j - 1) >> 1) & 1);

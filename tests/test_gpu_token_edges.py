@@ -38,3 +38,33 @@ def test_masses_of_flat_rows_of_the_largest_vocabulary(dc):
         else:
             want, p = pick(l[r].double().cpu().numpy(), float(u[r]), 1e3)
             assert got[r] == want and abs(share[r] - p) <= 2.0 ** -24 * p * 1.001, r
+
+
+# ---- attention: scores and values at the ends of their range ----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 20, 2.0 ** 25, 1e10, 2.0 ** 33, 1e30])
+@pytest.mark.parametrize("new", [1, 40, 300])
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (HF, 128)])
+def test_scores_far_beyond_fp32s_whole_numbers(dc, dtype, d, new, scale):
+    """One value of each key counts, and no two keys have the same (in the types' 8 bits, exactly): every other score lies far below the largest one a token sees,
+    so its output is that key's row of V, bit for bit."""
+    window = 100
+    c = Case(dc, new=(new,), start=(150,), d=d, H=4, Hkv=2, n_sink=3, window=window, dtype=dtype, seed=31, cu=new > 1)
+    g = torch.Generator(device="cuda").manual_seed(32)
+    keys, rows = c.seen_keys(0)
+    value = 1.0 + torch.randperm(128, generator=g, device="cuda")[torch.arange(len(keys), device="cuda") % 128].double() / 128      # distinct in any window and its first tokens
+    s = c.order[0]
+    c.k.zero_()
+    c.k[s][:, rows, 0] = value.to(dtype)
+    c.k[s][:, rows[:3], 0] = 0.5                        # (the first tokens, once they are out of the window)
+    q = torch.zeros(c.total, 4, d, dtype=dtype, device="cuda")
+    q[:, :, 0] = 1.0
+    out = c.cache.attend(q, c.batch, scale=scale)
+    key = torch.tensor(keys, device="cuda")
+    for t, at in enumerate(c.positions(0).tolist()):
+        seen = (key <= at) & (key > at - window)
+        best = torch.where(seen, value, -1.0).argmax()
+        want = c.v[s][:, rows[int(best)]].repeat_interleave(2, 0)
+        assert torch.equal(out[t], want), (t, at)
+    c.cache.check()
