@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(CH_THREADS, SPLIT ? 2 : 3) attend_chunk_kernel
         const float inv = 1.0f / l;
         uint32_t w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = Num<T>::pack(o[2 * i] * inv, o[2 * i + 1] * inv);
+        for (int i = 0; i < 8; ++i) w[i] = Num<T>::pack(Num<T>::mean(o[2 * i] * inv), Num<T>::mean(o[2 * i + 1] * inv));
         *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
         *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
       };
@@ -448,6 +448,7 @@ __global__ void __launch_bounds__(CH_THREADS, SPLIT ? 2 : 3) attend_chunk_kernel
       const float4 v = *reinterpret_cast<const float4*>(parts + slot * D + ((c ^ (slot & 15)) << 2));
       o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));
     }
-    *reinterpret_cast<uint2*>(out + (long long)tr * a.out_stride + (row - tr * G) * D + c * 4) = make_uint2(Num<T>::pack(o.x, o.y), Num<T>::pack(o.z, o.w));
+    *reinterpret_cast<uint2*>(out + (long long)tr * a.out_stride + (row - tr * G) * D + c * 4) = 
+        make_uint2(Num<T>::pack(Num<T>::mean(o.x), Num<T>::mean(o.y)), Num<T>::pack(Num<T>::mean(o.z), Num<T>::mean(o.w)));
   }
 }

@@ -28,6 +28,8 @@ template <> struct Num<bf16> {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
   }
+  // A weighted mean, its weights' sum off by their rounding: finite values have no mean beyond the type's largest.  (In bf16 the sums pass fp32's range before.)
+  static __device__ __forceinline__ float mean(float x) { return x; }
 };
 template <> struct Num<__half> {
   static constexpr bool is_bf16 = false;
@@ -38,6 +40,7 @@ template <> struct Num<__half> {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
   }
+  static __device__ __forceinline__ float mean(float x) { return fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.f), 65504.f) : x; }
 };
 
 // 16 bytes global -> shared, asynchronously; off: zeros, and the source is not read.

@@ -68,3 +68,23 @@ def test_scores_far_beyond_fp32s_whole_numbers(dc, dtype, d, new, scale):
         want = c.v[s][:, rows[int(best)]].repeat_interleave(2, 0)
         assert torch.equal(out[t], want), (t, at)
     c.cache.check()
+
+
+@pytest.mark.parametrize("new", [1, 40, 700])
+def test_values_at_fp16s_largest_stay_finite(dc, new):
+    """Rows of V of the type's largest value: a weighted mean of them is that value, never above."""
+    c = Case(dc, new=(new,), start=(900,), d=64, H=4, Hkv=2, window=512, dtype=HF, seed=41, cu=new > 1)
+    top = torch.finfo(HF).max
+    sign = torch.where(torch.arange(64, device="cuda") % 2 == 0, 1.0, -1.0)
+    c.v.copy_((top * sign).to(HF).expand_as(c.v))
+    q = (3 * torch.randn(c.total, 4, 64, generator=c.gen, device="cuda")).to(HF)
+    out = c.cache.attend(q, c.batch)
+    assert torch.isfinite(out).all()
+    c.check_attend(q, out, out)
+    # an infinity or a NaN that tokens see stays visible, in its column alone
+    keys, rows = c.seen_keys(0)
+    c.v[c.order[0], 0, rows[0], 0], c.v[c.order[0], 1, rows[1], 1] = float("inf"), float("nan")      # (first tokens)
+    q.zero_()
+    c.cache.attend(q, c.batch, out=out)
+    assert not torch.isfinite(out[:, :2, 0]).any() and torch.isnan(out[:, 2:, 1]).all() and torch.isfinite(out[:, :2, 1:]).all()
+    c.cache.check()
