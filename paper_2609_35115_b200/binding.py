@@ -177,6 +177,22 @@ def _cuda_stream_handle(stream) -> Optional[int]:
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _result(shape, dtype, device, stream):
+    """Memory for what a call returns: the current stream's, or that of the stream it is given, which writes it; the current stream may then be
+    using it when it is dropped."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream(device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    if stream.cuda_stream != here.cuda_stream:
+        out.record_stream(here)
+    return out
+
+
 class Snapshot:
     def __init__(self, lib, handle):
         self.lib, self.handle = lib, handle
@@ -506,8 +522,7 @@ class TokenCache:
         [n_tokens, heads, head_dim] (in q if given; qkv's own query columns may be given)."""
         n = batch.n_tokens
         if q is None:
-            import torch
-            q = torch.empty(n, self.c_cfg.n_heads, self.head_dim, dtype=self.dtype, device=self.device)
+            q = _result((n, self.c_cfg.n_heads, self.head_dim), self.dtype, self.device, stream)
         if batch.index != self._index or norm.index != self._index or norm.head_dim != self.head_dim:
             raise ValueError("the batch and the norm belong to another device or head_dim than the cache")
         x, xs = self._rows("qkv", qkv, self._qkv_width, n)
@@ -521,8 +536,7 @@ class TokenCache:
         """dc_cache_attend: q is [n_tokens, heads, head_dim] (or [n_tokens, heads * head_dim]); returns the outputs, in the shape of q."""
         n = batch.n_tokens
         if out is None:
-            import torch
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            out = _result(q.shape, self.dtype, self.device, stream)
         if batch.index != self._index:
             raise ValueError("the batch belongs to another device than the cache")
         x, xs = self._rows("q", q, self._q_width, n)
@@ -561,7 +575,7 @@ def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     if torch.cuda.current_device() != at:      # (the library launches on the current device)
         raise ValueError(f"logits: they are on device {at}, the current device is {torch.cuda.current_device()}")
     if tokens is None:
-        tokens = torch.empty(n, dtype=i32, device=logits.device)
+        tokens = _result((n,), i32, logits.device, stream)
     r = dc_sample_rules(_RULES_SIZE, _vector("temperature", temperature, f32, n, at), _vector("top_k", top_k, i32, n, at), _vector("top_p", top_p, f32, n, at),
                         _vector("min_p", min_p, f32, n, at))
     st = load_library().dc_sample_tokens(logits.data_ptr(), _dtype_code(logits), n, vocab, stride if n > 1 else max(stride, vocab), C.byref(r), _vector("u", u, f32, n, at),

@@ -88,3 +88,36 @@ def test_values_at_fp16s_largest_stay_finite(dc, new):
     c.cache.attend(q, c.batch, out=out)
     assert not torch.isfinite(out[:, :2, 0]).any() and torch.isnan(out[:, 2:, 1]).all() and torch.isfinite(out[:, :2, 1:]).all()
     c.cache.check()
+
+
+# ---- results that a call allocates itself ----------------------------------------------------------------------------------------------
+
+
+def behind_queued_work(like, call):
+    """What `call` returns while the current stream still holds queued writes to memory that it has given back."""
+    torch.cuda.synchronize()
+    held = [torch.empty_like(like) for _ in range(64)]
+    torch.cuda._sleep(200_000_000)
+    for t in held:
+        t.fill_(7)
+    del held, t
+    got = call()
+    torch.cuda.synchronize()
+    return got
+
+
+def test_results_on_another_stream_lie_in_memory_of_that_stream(dc):
+    side = torch.cuda.Stream()
+    c = Case(dc, new=(1,) * 6, start=(50,) * 6, d=128, H=8, Hkv=2, window=40, cu=False, seed=51)
+    q = c.normal(6, 8, 128)
+    want = c.cache.attend(q, c.batch)
+    assert torch.equal(behind_queued_work(want, lambda: c.cache.attend(q, c.batch, stream=side)), want)
+    assert torch.equal(behind_queued_work(want, lambda: c.cache.attend(q, c.batch, stream=side.cuda_stream)), want)      # a plain handle
+    qkv, norm = c.normal(6, 12 * 128), dc.QKNorm(torch.ones(128, device="cuda"), torch.ones(128, device="cuda"))
+    want = c.cache.append(qkv, c.batch, norm)
+    assert torch.equal(behind_queued_work(want, lambda: c.cache.append(qkv, c.batch, norm, stream=side)), want)
+    logits, u = torch.randn(6, 1000, device="cuda"), torch.full((6,), 0.5, device="cuda")
+    want = dc.sample_tokens(logits, u)
+    assert torch.equal(behind_queued_work(want, lambda: dc.sample_tokens(logits, u, stream=side)), want)
+    assert torch.equal(dc.sample_tokens(logits, u, stream=0), want)
+    c.cache.check()
