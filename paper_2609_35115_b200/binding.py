@@ -269,7 +269,7 @@ class Stream:
         T = feats.shape[0]
         if out is None:
             n = max(T, 0) * self.model.out_per_frame
-            out = torch.empty(max(n, 1), dtype=torch.float32, device=feats.device)
+            out = _result((max(n, 1),), torch.float32, feats.device, stream)
         n_out = C.c_int(0)
         st = self.lib.dc_decode_chunk(self.handle, feats.data_ptr(), T, out.data_ptr(), C.byref(n_out),
                                       _cuda_stream_handle(stream))
@@ -286,7 +286,7 @@ class Stream:
         assert feats.is_cuda and feats.dtype == torch.float32 and feats.is_contiguous()
         n = feats.shape[0]
         if out is None:
-            out = torch.empty(n * self.model.out_per_frame, device=feats.device, dtype=torch.float32)
+            out = _result((n * self.model.out_per_frame,), torch.float32, feats.device, stream)
         n_out = C.c_longlong(0)
         st = self.lib.dc_decode_wavefront(self.handle, feats.data_ptr(), n, out.data_ptr(), C.byref(n_out),
                                           _cuda_stream_handle(stream))
@@ -385,7 +385,7 @@ def decode_wavefront_batch(model: Model, streams: Sequence[Stream], feats, outs=
     import torch
     n = len(streams)
     if outs is None:
-        outs = [torch.empty(f.shape[0] * model.out_per_frame, device=f.device, dtype=torch.float32) for f in feats]
+        outs = [_result((f.shape[0] * model.out_per_frame,), torch.float32, f.device, stream) for f in feats]
     for f in feats:
         assert f.is_cuda and f.dtype == torch.float32 and f.is_contiguous()
     hs = (C.c_void_p * n)(*[s.handle for s in streams])

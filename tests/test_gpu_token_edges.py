@@ -121,3 +121,20 @@ def test_results_on_another_stream_lie_in_memory_of_that_stream(dc):
     assert torch.equal(behind_queued_work(want, lambda: dc.sample_tokens(logits, u, stream=side)), want)
     assert torch.equal(dc.sample_tokens(logits, u, stream=0), want)
     c.cache.check()
+
+
+def test_decoded_audio_on_another_stream_lies_in_memory_of_that_stream(dc):
+    import dc_workloads as wl
+    cfg = wl.tiny_flow(name="elsewhere", n_chunks=3, seed=5)
+    w = wl.make_workload(cfg)
+    m, side = dc.Model(cfg, w.weights, max_batch=cfg.n_steps), torch.cuda.Stream()
+    st = m.open_stream()
+    feats = torch.from_numpy(np.ascontiguousarray(w.streams[0].feats[:2 * cfg.f_chunk])).cuda()
+    for call in (lambda s: st.decode_chunk(feats[:cfg.f_chunk], stream=s), lambda s: st.decode_wavefront(feats, stream=s), lambda s: dc.decode_wavefront_batch(m, [st], [feats], stream=s)[0]):
+        st.reset()
+        want = call(None)
+        torch.cuda.synchronize()
+        st.reset()
+        assert torch.equal(behind_queued_work(want, lambda: call(side)), want)
+    st.close()
+    m.destroy()
