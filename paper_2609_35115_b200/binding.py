@@ -514,7 +514,7 @@ class TokenCache:
         st, d = t.stride(), self.head_dim
         if t.dtype is self.dtype and t.get_device() == self._index and (
                 (len(st) == 3 and t.shape == (n, width // d, d) and st[1] == d and st[2] == 1) or (len(st) == 2 and t.shape == (n, width) and st[1] == 1)):
-            return t.data_ptr(), st[0] if n > 1 else max(st[0], width)
+            return t.data_ptr(), st[0] if n > 1 else (max(st[0], width) + 7) & ~7      # (one row: any multiple of 8 will do)
         raise ValueError(f"{name}: {n} rows of {width} {self.dtype} values on {self.device} are wanted, not {tuple(t.shape)} (strides {st}) {t.dtype} on {t.device}")
 
     def append(self, qkv, batch: TokenBatch, norm: QKNorm, q=None, stream=None):

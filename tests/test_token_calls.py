@@ -52,3 +52,22 @@ def test_logits_of_another_device_than_the_current_one_are_not_sampled(monkeypat
         with pytest.raises(ValueError, match="current device"):
             binding.sample_tokens(logits, u, tokens=tokens, stream=0)
         assert not lib.calls
+
+
+class Rows(OnDevice):
+    """A matrix whose rows are `apart` values apart."""
+
+    def __init__(self, n, width, apart):
+        super().__init__(n, width, dtype=torch.bfloat16)
+        self.apart = apart
+
+    def stride(self):
+        return self.apart, 1
+
+
+# the stride of a single row counts for nothing: it may be that of any matrix which the row was taken from
+@pytest.mark.parametrize("n,apart,want", [(1, 260, 264), (1, 256, 256), (1, 3, 256), (1, 1000, 1000), (2, 260, 260), (2, 264, 264)])
+def test_rows_of_a_single_token_lie_any_number_of_values_apart(n, apart, want):
+    c = binding.TokenCache.__new__(binding.TokenCache)
+    c.handle, c.dtype, c._index, c.head_dim, c.device = None, torch.bfloat16, 0, 64, "cuda:0"
+    assert c._rows("q", Rows(n, 256, apart), 256, n) == (0x10000, want)
