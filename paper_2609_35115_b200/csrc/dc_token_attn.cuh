@@ -101,7 +101,7 @@ __device__ __noinline__ void plain_row(const AttendArgs& a, const uint8_t* sQ, i
           dot = fma2(Num<T>::unpack(x.z), Num<T>::unpack(y.z), dot);
           dot = fma2(Num<T>::unpack(x.w), Num<T>::unpack(y.w), dot);
         }
-        const float s = (dot.x + dot.y) * a.scale_log2e;
+        const float s = __fmul_rn(dot.x + dot.y, a.scale_log2e);
         if (pass == 0) {
           top = fmaxf(top, s);
         } else {

@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(WARPS * 32) attend_step_kernel(const AttendArg
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             float& y = sc[h][mt][2 * k + i];
-            y = mt * 16 + 8 * k + g < n ? y * a.scale_log2e : -INFINITY;
+            y = mt * 16 + 8 * k + g < n ? __fmul_rn(y, a.scale_log2e) : -INFINITY;      // (rounded here, whatever is taken off below)
             x = fmaxf(x, y);
           }
 #pragma unroll
