@@ -89,6 +89,7 @@ __device__ __forceinline__ unsigned long long cluster_sum(const unsigned long lo
 }
 __device__ __forceinline__ void cluster_or_block_sync(int splits) {
   if (splits > 1) {
+    __syncwarp();      // (the cluster's barrier is met by whole warps)
     ptx::cluster_arrive();
     ptx::cluster_wait();
   } else {
@@ -673,6 +674,7 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
       pull_few<NT>(c, sh.hist[buf], count, few, a.splits);
     }
     if (a.splits > 1) {
+      __syncwarp();
       ptx::cluster_arrive();
       if (rank != 0) {
         ptx::cluster_wait();
@@ -725,6 +727,7 @@ __global__ void __launch_bounds__(STREAM ? SMP_WIDE : SMP_THREADS, STREAM ? 2 : 
         if (a.probs) a.probs[row_i] = (float)(w.value(logit_of((uint32_t)(me >> 32))) / ((double)sh.above / (double)ONE));
       }
     }
+    __syncwarp();
     if (a.splits > 1) ptx::cluster_wait();      // the others read this CTA's count of candidates: its memory stays until all of them have arrived (they have, long ago)
     return;
   }

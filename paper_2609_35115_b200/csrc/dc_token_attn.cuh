@@ -405,6 +405,7 @@ __global__ void __launch_bounds__(CH_THREADS, SPLIT ? 2 : 3) attend_chunk_kernel
   ptx::tc_fence_before();
   __syncthreads();
   if (warp == 5) ptx::tmem_dealloc(tmem, CH_TMEM);
+  __syncwarp();               // (the cluster's barrier is met by whole warps)
   ptx::cluster_arrive();      // every CTA of the cluster is through with its K and V: the parts go there
   ptx::cluster_wait();
   if (warp < 4 && !failed) {
@@ -426,6 +427,7 @@ __global__ void __launch_bounds__(CH_THREADS, SPLIT ? 2 : 3) attend_chunk_kernel
       st_cluster(ptx::map_to_cta(ptx::smem_u32(&bars.l[slot]), to), l);
     }
   }
+  __syncwarp();
   ptx::cluster_arrive();
   ptx::cluster_wait();      // (nobody reads or writes another CTA's memory behind this)
   const int r0 = rank * own, mine_n = min(own, n_rows - r0);

@@ -541,6 +541,7 @@ __global__ void __launch_bounds__(WARPS * 32) attend_step_kernel(const AttendArg
     }
   }
   if (a.splits == 1) return;
+  __syncwarp();      // (the cluster's barrier is met by whole warps)
   ptx::cluster_arrive();
   ptx::cluster_wait();
   const uint32_t all_s = ptx::smem_u32(all), cm_s = ptx::smem_u32(cm), cl_s = ptx::smem_u32(cl);
@@ -562,6 +563,7 @@ __global__ void __launch_bounds__(WARPS * 32) attend_step_kernel(const AttendArg
     const float inv = 1.0f / L;
     *reinterpret_cast<uint32_t*>(out + e) = Num<T>::pack(x * inv, y * inv);
   }
+  __syncwarp();
   ptx::cluster_arrive();      // no CTA's shared memory goes while another reads it
   ptx::cluster_wait();
 }

@@ -47,3 +47,14 @@ def test_tensor_memory_is_given_back_before_a_cta_waits_for_its_cluster():
     body = kernel("dc_token_attn.cuh", "attend_chunk_kernel")
     assert body.rindex("tmem_dealloc") < body.index("cluster_arrive") < body.index("cluster_wait")
     assert body.rindex("tmem_ld64(lane_base + CH_O") < body.index("cluster_arrive")
+
+
+@pytest.mark.parametrize("file,name", [("dc_token_attn.cuh", "attend_chunk_kernel"), ("dc_token_cache.cu", "attend_step_kernel"), ("dc_sample.cu", "sample_kernel")])
+def test_whole_warps_meet_at_the_cluster_barriers(file, name):
+    """Behind branches that a warp's lanes may have taken apart they come together before they arrive."""
+    with open(os.path.join(CSRC, file)) as f:
+        text = re.sub(r"//[^\n]*", "", f.read())
+    arrivals = [m.start() for m in re.finditer(r"ptx::cluster_arrive\(\);", text)]
+    assert arrivals and "cluster_arrive" in (kernel(file, name) if name != "sample_kernel" else text)
+    for at in arrivals:
+        assert re.search(r"__syncwarp\(\);\s*$", text[:at]), text[max(0, at - 200):at]
