@@ -430,7 +430,7 @@ dc_status dc_selftest_bounded_wait(int max_polls);
  * first n_sink positions, which are never evicted, and n_sink + (p - n_sink) mod ring_rows behind them.  A token at position q sees
  * position p if p <= q and (p < n_sink or p > q - window).  A call brings up to ring_rows - window + 1 tokens of a sequence (their
  * rows must not evict what the first of them sees); longer input is given in pieces.  Rows that no token of a call sees may hold
- * anything, infinities and NaN included. */
+ * anything, infinities and NaN included; in a row that a token sees they can make the token's outputs infinite or NaN. */
 typedef struct dc_cache dc_cache;
 
 typedef struct dc_cache_config {
@@ -447,10 +447,10 @@ typedef struct dc_cache_config {
 /* The sequences of one call.  Sequence i is session sessions_dev[i] (NULL: i); its tokens are the rows cu_tokens_dev[i] ..
  * cu_tokens_dev[i + 1] - 1 of the call's matrices, at positions start_dev[i], start_dev[i] + 1, ...  Without
  * cu_tokens_dev (NULL) sequence i is row i: one token each (n_tokens == n_seqs, max_tokens == 1).  n_tokens is the number of
- * rows of the matrices, max_tokens the most that one sequence brings.  Rows behind the last sequence are padding: nothing is read or
- * written there.  The device arrays are read when the work runs; a sequence whose values do not fit (a session
+ * rows of the matrices, max_tokens the most that one sequence brings.  Rows behind the last sequence are padding: nothing is
+ * written there, and what they hold counts for nothing.  The device arrays are read when the work runs; a sequence whose values do not fit (a session
  * that the cache does not have, a negative position, more tokens than max_tokens or than the ring takes, rows outside of the
- * matrices) is left out as if it had no tokens.  The sessions of a dc_cache_append call must be distinct. */
+ * matrices) is left out as if it had no tokens: its output rows stay as they were, and no call reports it.  The sessions of a dc_cache_append call must be distinct. */
 typedef struct dc_token_batch {
   uint32_t       size;           /* sizeof(dc_token_batch)                                       */
   int32_t        n_seqs, n_tokens, max_tokens;
@@ -492,8 +492,10 @@ dc_status dc_cache_append(dc_cache* cache, const dc_token_batch* batch, const dc
 
 /* Attention of the batch's tokens, whose own keys and values have been appended, over their sessions' rows:
  * out = sum_p w_p v_p / sum_p w_p with w_p = exp(scale * <q, k_p>) over the positions p that the token sees; query head h
- * reads key/value head h / (n_heads / n_kv_heads).  Scores, sums and outputs are held in fp32 until the one rounding of the result; in
- * calls of several tokens the numerators are rounded to the cache's type before the product with v.  0 < scale <= 1e30.
+ * reads key/value head h / (n_heads / n_kv_heads).  Scores, sums and outputs are held in fp32 until the rounding of the result.  Before the product
+ * with v the numerators are rounded: in calls of several tokens to the cache's type, in calls of single tokens to two values of that type, one holding what the
+ * other leaves (16 bits in bf16; in fp16 22, and none below 2^-25 of the largest numerator).  Sums of numerators times v are fp32's: values of a bf16 cache from about 1e26 on
+ * can pass its range.  0 < scale <= 1e30; in calls of several tokens scores beyond 2^24 are right but slow.
  *   q_dev, out_dev : [n_tokens] rows of n_heads * head_dim values, q_stride / out_stride values apart (multiples of 8).  No overlap with
  *                    each other or with the cache. */
 dc_status dc_cache_attend(dc_cache* cache, const dc_token_batch* batch, const void* q_dev, long long q_stride, float scale,
@@ -503,9 +505,9 @@ dc_status dc_cache_attend(dc_cache* cache, const dc_token_batch* batch, const vo
  *   z_i = (l_i - max l) / temperature, w_i = exp(z_i), in the order of descending l, ties by lowest index, kept are in turn
  *     top-k : the first top_k tokens                                           (top_k < 1: all)
  *     top-p : the shortest beginning of those whose mass reaches top_p times the mass that top-k left, one token at least   (top_p >= 1: all)
- *     min-p : those of them with w_i >= min_p                                  (min_p <= 0: all)
+ *     min-p : those of them with w_i >= min_p                                  (min_p <= 0: all; above 1: as for 1)
  *   token = the first kept index, in the vocabulary's order, whose running mass exceeds u times the kept mass (u >= 1: the last kept one).
- * temperature <= 0 (or NaN): the lowest index of the largest logit.  NaN logits count as -infinity, which is never chosen; a row without
+ * temperature <= 0 (or NaN): the lowest index of the largest logit; a NaN as top_p or min_p: all.  NaN logits count as -infinity, which is never chosen; a row without
  * any other has token -1, probability 0; +infinity outweighs everything finite.  Weights are held in fp64 and their masses as
  * exact multiples of 2^-45 of the largest weight: the result depends on nothing but the row.
  *   logits_dev : [n_rows] rows of vocab logits (DC_F32, DC_BF16 or DC_F16), row_stride >= vocab values apart, 16-byte aligned (the rows behind the

@@ -10,7 +10,7 @@
 // border that close to a row's random number is met once in millions of rows.
 //
 // Bound by the latency of the passes and of the cluster's barriers between them (few rows), by the passes' instructions, fp64 and shared-memory adds
-// among them (many).  Measured, 256 rows of 131,072 fp32 logits: greedy 37 us, no rule 106 us, top-k 50 85 us, top-p 0.9 247 us; 48 rows of 32,001: 10, 12, 15, 27 us; one
+// among them (many; the streamed form, two CTAs of 512 threads an SM, has 64 registers a thread and spills 16 to 72 bytes).  Measured, 256 rows of 131,072 fp32 logits: greedy 37 us, no rule 106 us, top-k 50 85 us, top-p 0.9 247 us; 48 rows of 32,001: 10, 12, 15, 27 us; one
 // of 4,097: 8 to 10 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -926,7 +926,7 @@ extern "C" dc_status dc_sample_tokens(const void* logits_dev, int dtype, int n_r
   SampleArgs a{logits_dev, row_stride, vocab, 0, 1, rules->temperature_dev, rules->top_p_dev, rules->min_p_dev, u_dev, rules->top_k_dev, tokens_dev, probs_dev};
   // Rows enough for every SM: a CTA streams its row, of a long row two, so that the rows under way stay in the L2 cache from one pass to the next (256 rows
   // of 131,072, top-k of 50: 107 us in one, 84 us in two, 100 us in four, 139 us in shared memory).  Else the row lies in the shared memory of a cluster: as many CTAs as its logits need, and while SMs are
-  // idle more, down to 4096 logits each.
+  // idle twice as many as long as one has more than 4,096 logits (4,097 become 2 x 2,049; one CTA against two at that border has not been measured).
   const bool stream = n_rows >= n_sm && vocab > SMP_SLICE;
   if (stream) {
     a.splits = vocab > 4 * SMP_SLICE ? 2 : 1;

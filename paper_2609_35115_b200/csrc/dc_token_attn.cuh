@@ -13,13 +13,14 @@
 // The running maximum moves only when a row's new maximum exceeds it by 8 (in powers of two): the numerators then stay below 2^8,
 // within fp16 too, and the output in tensor memory is rescaled in few of the steps.
 //
-// Measured: 8,192 tokens, 16 query heads over 4 of 128 values, window 2,048: 148 us in short bursts (814 TFLOP/s of what the masks leave), 164 us under
-// lasting load, where the clock falls with the power.  A step of 64 rows takes a CTA 1,650 cycles with another on its SM: the tensor core is busy for 1,280 of them.
+// Measured: 8,192 tokens, 16 query heads over 4 of 128 values, window 2,048: 145 us in short bursts (831 TFLOP/s of what the masks leave), 163 us under
+// lasting load, where the clock falls with the power.  A step of 64 rows takes a CTA 1,650 cycles with another on its SM; both CTAs' products hold the tensor pipe for 58 % of
+// the cycles (40 % by the counter of its arithmetic: a product of 64 columns takes more than its share), the exponentials their unit for 44 %.
 
 constexpr int CH_M = 128, CH_N = STEP_N, CH_STAGES = 2, CH_THREADS = 192;
 constexpr uint32_t CH_TMEM = 256, CH_O = 128;   // columns: scores at 0 and 64, output at 128
 
-// Never less than a third of an SM's: with three CTAs on an SM the third would wait for tensor memory while its cluster waits for it.
+// Never less than a third of an SM's: a third CTA on an SM would wait for tensor memory, and its cluster for it.
 template <int D>
 constexpr size_t chunk_smem() {
   const size_t need = 1024 + (size_t)CH_M * D * 2 + (size_t)CH_STAGES * 2 * CH_N * D * 2;

@@ -293,10 +293,10 @@ constexpr int step_smem(int warps) { return warps * STEP_STAGES * STEP_UNIT; }
 // columns of V, as their 16 rows and the query heads that share a K/V head as their 8 columns (NH = 2: twice 8): a row is read once for
 // all of them, and a group of up to 8 heads takes 8 + 16 products a unit.  (With the heads as the 16 rows it took 48, and
 // those, at about 35 cycles each, bounded the kernel: 36 us against 20 for one session of 32,768 rows.)  Measured: 48 sessions of up to 4,100 rows, 8 x 128 values of K and of V each,
-// 98 us, 6.4 TB/s; one session of 32,768 rows, 4 heads, 20 us, 3.3 TB/s: its four clusters sit in four of the device's eight GPCs.  The units of a
+// 98 us in short bursts, 6.4 TB/s, 103 us among other calls; one session of 32,768 rows, 4 heads, 20 us, 3.3 TB/s: its four clusters sit in four of the device's eight GPCs.  The units of a
 // (sequence, head) are dealt out over the warps of a cluster of CTAs, which joins the partial results through distributed shared
-// memory: no workspace, no second launch.  The numerators enter the second product as two halves (their rounding to 16 bits and what
-// that leaves), so that the result is rounded once.
+// memory: no workspace, no second launch.  The numerators enter the second product as two values of the cache's type (their rounding and what
+// that leaves: 16 bits in bf16, 22 in fp16 down to 2^-25), so that the rounding of the result is the one that counts.
 template <typename T, int D, int NH, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32) attend_step_kernel(const AttendArgs a) {
   constexpr int UN = STEP_HALF / (2 * D);    // rows of a unit

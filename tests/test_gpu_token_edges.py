@@ -138,3 +138,16 @@ def test_decoded_audio_on_another_stream_lies_in_memory_of_that_stream(dc):
         assert torch.equal(behind_queued_work(want, lambda: call(side)), want)
     st.close()
     m.destroy()
+
+
+def test_rules_that_are_no_numbers_or_out_of_range(dc):
+    """A NaN as top_p or min_p rules nothing out; min_p above 1 is as 1: the logits that tie with the largest."""
+    g = torch.Generator(device="cuda").manual_seed(61)
+    for vocab in (50, 9000):
+        l, u = torch.round(torch.randn(40, vocab, generator=g, device="cuda") * 2), torch.rand(40, generator=g, device="cuda")
+        every = lambda x: torch.full((40,), x, device="cuda")
+        free = dc.sample_tokens(l, u)
+        assert torch.equal(dc.sample_tokens(l, u, top_p=every(float("nan"))), free) and torch.equal(dc.sample_tokens(l, u, min_p=every(float("nan"))), free)
+        best = dc.sample_tokens(l, u, min_p=every(1.0))
+        assert torch.equal(dc.sample_tokens(l, u, min_p=every(7.0)), best)
+        assert torch.equal(l.gather(1, best.long()[:, None])[:, 0], l.amax(1))
