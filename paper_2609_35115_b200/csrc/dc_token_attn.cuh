@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(CH_THREADS, SPLIT ? 2 : 3) attend_chunk_kernel
       const float4 v = *reinterpret_cast<const float4*>(parts + slot * D + ((c ^ (slot & 15)) << 2));
       o = make_float4(fmaf(f, v.x, o.x), fmaf(f, v.y, o.y), fmaf(f, v.z, o.z), fmaf(f, v.w, o.w));
     }
-    *reinterpret_cast<uint2*>(out + (long long)tr * a.out_stride + (row - tr * G) * D + c * 4) = 
+    *reinterpret_cast<uint2*>(out + (long long)tr * a.out_stride + (row - tr * G) * D + c * 4) =
         make_uint2(Num<T>::pack(Num<T>::mean(o.x), Num<T>::mean(o.y)), Num<T>::pack(Num<T>::mean(o.z), Num<T>::mean(o.w)));
   }
 }
